@@ -50,8 +50,12 @@ extern "C" {
 #define DIT_ATTN_ERR_CAPACITY      (-8)  /* output buffer of dit_attn_plan too small */
 #define DIT_ATTN_ERR_KERNEL        (-9)  /* dit_attn_set_kernel: no such kernel */
 #define DIT_ATTN_ERR_PARTS         (-10) /* dit_attn_merge: n_parts outside 1..8 */
-#define DIT_ATTN_ERR_LIMIT         (-11) /* dit_attn_varlen_fwd_noalloc: the pack exceeds the fixed scratch limits */
+#define DIT_ATTN_ERR_LIMIT         (-11) /* dit_attn_varlen_fwd_noalloc: the pack exceeds the fixed scratch limits; elsewhere: more rows than a launch takes */
 #define DIT_ATTN_ERR_CAPTURE       (-12) /* the stream is capturing and the call would have to allocate or copy */
+#define DIT_ATTN_ERR_MASK          (-13) /* dit_attn_mask: a field out of range, or one without the one it belongs to */
+#define DIT_ATTN_ERR_ROPE          (-14) /* dit_attn_rope, rot_dim or layout out of range */
+#define DIT_ATTN_ERR_NORM          (-15) /* no such norm, eps out of range, or weights without a norm */
+#define DIT_ATTN_ERR_STRIDE        (-16) /* a row stride that is no multiple of 8, too short for a row or too long */
 
 typedef struct dit_attn_ctx dit_attn_ctx; /* opaque */
 
@@ -195,6 +199,124 @@ int dit_attn_sp_unpack_heads(dit_attn_ctx* ctx, const void* src, void* dst, int6
                              int32_t n_heads, int32_t head_dim, int32_t sp_degree, void* stream);
 
 /*
+ * Rotation table of token positions: what dit_attn_qk_norm_rope turns queries and keys by.  A DiT's tokens have positions on
+ * several axes (text; frame, row, column), each of which rotates a share of a head's elements.  The table is a function of the
+ * positions alone: made once for a pack, it serves every block of every denoising step.
+ *     table[r, pair] = magnitude * (cos, sin)(positions[r, axis of pair] * f(pair))
+ * The pairs of axis 0 come first.  With d = axis_dim[a] elements (d / 2 pairs j) and base theta[a]:
+ *     DIT_ATTN_ROPE_PLAIN    f = theta^(-2j/d)
+ *     DIT_ATTN_ROPE_LINEAR   f = theta^(-2j/d) / factor                    positions squeezed into the trained range
+ *     DIT_ATTN_ROPE_BASE     f = (theta * factor^(d/(d-2)))^(-2j/d)        fast pairs kept, slow ones squeezed (d = 2: plain)
+ *     DIT_ATTN_ROPE_BANDS    f = theta^(-2j/d) * (g + (1-g) / factor),     pairs that turn `high` times and more over
+ *                            g = clamp((turns - low) / (high - low)),      original_length kept, those under `low` squeezed,
+ *                            turns = original_length * theta^(-2j/d) / 2pi   a blend in between
+ * Angles are computed in double precision: any int32 position has a table entry within a few units of fp32 rounding.
+ *   positions  DEVICE int32 [n_rows, n_axes], contiguous.      n_rows >= 0 (0: nothing is launched).
+ *   rope       HOST, read during the call.
+ *   table      DEVICE fp32 [n_rows, sum of axis_dim / 2, 2] (cos, sin), 16-byte aligned.
+ * Enqueues one kernel on `stream`; allocates nothing.  Returns DIT_ATTN_OK, _ERR_NULL, _ROPE, _CU_SEQLENS (n_rows < 0), _ALIGN,
+ * _LIMIT (over 2^34 rows) or _HIP.
+ */
+#define DIT_ATTN_ROPE_PLAIN   0
+#define DIT_ATTN_ROPE_LINEAR  1
+#define DIT_ATTN_ROPE_BASE    2
+#define DIT_ATTN_ROPE_BANDS   3
+typedef struct dit_attn_rope {
+  int32_t n_axes;              /* 1..4 */
+  int32_t scaling;             /* DIT_ATTN_ROPE_PLAIN .. DIT_ATTN_ROPE_BANDS */
+  int32_t axis_dim[4];         /* rotated elements of an axis: even, at least 2; at most 128 together */
+  double theta[4];             /* base of an axis, at least 1 */
+  double factor[4];            /* at least 1; not read with DIT_ATTN_ROPE_PLAIN */
+  double original_length[4];   /* DIT_ATTN_ROPE_BANDS: positions of the trained range */
+  double low, high;            /* DIT_ATTN_ROPE_BANDS: low < high */
+  double magnitude;            /* multiplies both values; 1 for a rotation */
+} dit_attn_rope;
+int dit_attn_rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_rows, const dit_attn_rope* rope,
+                        float* table, void* stream);
+
+/*
+ * Norm of queries and keys for each head and rotation by position in one pass, as a DiT block does right before its attention
+ * (paper Section 2.1: the denoising steps' attention over text and latent tokens).  For each row and head, in fp32:
+ *     DIT_ATTN_NORM_RMS     y = x * rsqrt(mean(x^2) + eps) * weight + bias
+ *     DIT_ATTN_NORM_LAYER   y = (x - mean(x)) * rsqrt(var(x) + eps) * weight + bias       (var: mean of squares)
+ *     DIT_ATTN_NORM_NONE    y = x
+ * then the first rot_dim elements are turned in pairs, (a, b) -> (a cos - b sin, b cos + a sin) with the row's table entry of
+ * the pair, and the result is rounded once to bf16.  Pair j is
+ *     DIT_ATTN_ROPE_INTERLEAVED  (2j, 2j + 1)          DIT_ATTN_ROPE_HALF  (j, j + rot_dim / 2)
+ *   q, k        HOST structures, read during the call; one of them may be NULL (only the other side is done).
+ *     x, out    DEVICE bf16, n_rows rows of n_heads * head_dim elements, 16-byte aligned, row_stride / out_row_stride elements
+ *               apart (0: contiguous; a multiple of 8).  So x may lie in the output of a fused projection.  out == x (with equal
+ *               strides) replaces the rows in place; otherwise no out overlaps any input.
+ *     weight, bias  DEVICE fp32 [head_dim], 16-byte aligned, or NULL (1 and 0).
+ *   n_rows      >= 0 (0: nothing is launched).      head_dim  64 or 128.      eps  finite, not negative.
+ *   table       DEVICE fp32 [n_rows, rot_dim / 2, 2] (cos, sin) as dit_attn_rope_table writes it, 16-byte aligned; not read with
+ *               rot_dim == 0.
+ *   rot_dim     rotated elements of a head, a multiple of 8 up to head_dim; the others are only normed.
+ * Enqueues one kernel on `stream`; allocates nothing.  Returns DIT_ATTN_OK, _ERR_NULL, _HEAD_DIM, _N_HEADS, _NORM, _ROPE,
+ * _STRIDE, _CU_SEQLENS (n_rows < 0), _ALIGN, _LIMIT or _HIP.
+ */
+#define DIT_ATTN_NORM_NONE          0
+#define DIT_ATTN_NORM_RMS           1
+#define DIT_ATTN_NORM_LAYER         2
+#define DIT_ATTN_ROPE_INTERLEAVED   0
+#define DIT_ATTN_ROPE_HALF          1
+typedef struct dit_attn_norm_heads {
+  const void* x;
+  void* out;
+  int64_t row_stride, out_row_stride;
+  const float* weight;
+  const float* bias;
+  int32_t n_heads;             /* 1..65535 */
+} dit_attn_norm_heads;
+int dit_attn_qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const dit_attn_norm_heads* k, int64_t n_rows,
+                          int32_t head_dim, int32_t norm, float eps, const float* table, int32_t rot_dim, int32_t layout,
+                          void* stream);
+
+/*
+ * Attention with masks, capped scores and a distance bias, over a pack with separate query and key boundaries and key heads
+ * shared by groups of query heads.  Row i of a sequence with lq queries and lk keys has position pos = i + lk - lq (its
+ * queries are the last of its keys: one new token has lq = 1); head h reads key head h / (n_heads / n_kv_heads).
+ *     s = scale * <q, k_j>;   softcap C > 0: s = C * tanh(s / C);   slopes: s = s - slopes[h] * |pos - j|
+ *     key j is seen  iff  (not causal, or j <= pos, or j < prefix of the sequence)
+ *                     and (no ids, or q_doc of the row == k_doc of the key, and that id is not negative)
+ *     out = sum over seen keys exp(s - lse) v_j,     lse = ln sum over seen keys exp(s)
+ * A row that sees no key gets 0 and -inf.  What lies in keys and values that a row does not see (NaN and infinities too) has no
+ * effect on it.  So a padded batch gives its padding rows negative ids, several documents of a sequence get an id each (in any
+ * order), and text that all of an ordered sequence sees is its prefix.
+ *   q           DEVICE bf16 [Tq, n_heads, head_dim];  k, v  DEVICE bf16 [Tk, n_kv_heads, head_dim];  16-byte aligned.
+ *   row_strides HOST, elements from row to row of q, k and v (multiples of 8, at most 2^24), or NULL: contiguous.  The heads of a
+ *               row are contiguous.
+ *   cu_seqlens_q, cu_seqlens_k   HOST, as dit_attn_cross_varlen_fwd; cu_seqlens_k may be NULL: keys share the query boundaries.
+ *               Any number of sequences.
+ *   n_kv_heads  divides n_heads.      head_dim  64 or 128.      scale  finite.
+ *   mask        HOST structure, read during the call, or NULL: every key is seen.
+ *   out         DEVICE bf16 [Tq, n_heads, head_dim], contiguous, overlapping no input.  Exactly the rows [0, Tq) are written.
+ *   lse         DEVICE fp32 [Tq, n_heads] or NULL.  Its sum is taken over fp32 probabilities (the products with v take them as
+ *               bf16, and out is divided by the sum of those).
+ * The call reads no work-list and builds none: boundaries travel with the kernel.  Sequences with few rows or packs with few
+ * items have their keys split over the compute units and the parts joined by a second kernel, in a fixed order (the same pack
+ * gives the same bits; a sequence's bits depend on what it is packed with).  The parts, and the id ranges of key tiles, lie in
+ * the context's workspace, which grows with hipMalloc when a call needs more (DIT_ATTN_ERR_CAPTURE on a capturing stream: call
+ * once outside the capture first).  As with every use of a context, calls and replays of captured calls that use the workspace
+ * must not overlap.
+ * Returns DIT_ATTN_OK, _ERR_NULL, _HEAD_DIM, _N_HEADS, _CU_SEQLENS, _SCALE, _MASK, _STRIDE, _ALIGN, _LIMIT (2^31 work items),
+ * _CAPTURE or _HIP; validation precedes any launch.
+ */
+typedef struct dit_attn_mask {
+  int32_t causal;              /* 0 or 1 */
+  float softcap;               /* C, or 0: scores are not capped */
+  const int32_t* prefix;       /* HOST [n_seqs], not negative, with causal = 1; or NULL: 0 */
+  const float* slopes;         /* DEVICE fp32 [n_heads], or NULL: no bias */
+  const int32_t* q_doc;        /* DEVICE int32 [Tq] and [Tk], or both NULL */
+  const int32_t* k_doc;
+} dit_attn_mask;
+int dit_attn_masked_varlen_fwd(dit_attn_ctx* ctx,
+                               const void* q, const void* k, const void* v, const int64_t* row_strides,
+                               const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t n_seqs,
+                               int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                               const dit_attn_mask* mask, void* out, float* lse, void* stream);
+
+/*
  * Kernel choice of a context.  The library has two kernels for the same
  * operation (which one is fastest depends on the pack, Section 4.3 / Table 3:
  * image steps are short, video steps long):
@@ -242,7 +364,7 @@ int dit_attn_set_kernel(dit_attn_ctx* ctx, int kernel);
  * results and their log-sum-exp in a workspace owned by the context (grown with hipMalloc when a call needs more), and one
  * merge kernel on the same stream writes `out`.  Off (max_splits = 1) by default, because it changes the summation order: with it
  * a sequence's bits depend on what it is packed with (they stay within the same tolerance of the exact result).
- * Applies to every forward entry point.  Returns DIT_ATTN_OK, DIT_ATTN_ERR_NULL or DIT_ATTN_ERR_PARTS (outside 1..8).
+ * Applies to every forward entry point but dit_attn_masked_varlen_fwd, which splits by itself.  Returns DIT_ATTN_OK, DIT_ATTN_ERR_NULL or DIT_ATTN_ERR_PARTS (outside 1..8).
  */
 int dit_attn_set_split_kv(dit_attn_ctx* ctx, int max_splits);
 

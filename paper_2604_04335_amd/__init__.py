@@ -29,6 +29,21 @@ __all__ = [
     "dit_attn_merge",
     "dit_attn_sp_pack_heads",
     "dit_attn_sp_unpack_heads",
+    "dit_attn_rope_table",
+    "dit_attn_qk_norm_rope",
+    "dit_attn_masked_varlen_fwd",
+    "RopeSpec",
+    "NormHeads",
+    "AttnMask",
+    "ROPE_PLAIN",
+    "ROPE_LINEAR",
+    "ROPE_BASE",
+    "ROPE_BANDS",
+    "ROPE_INTERLEAVED",
+    "ROPE_HALF",
+    "NORM_NONE",
+    "NORM_RMS",
+    "NORM_LAYER",
     "dit_sched_laxity",
     "dit_sched_plan_round",
     "SchedCandidate",
@@ -63,6 +78,10 @@ ERROR_NAMES = {
     -10: "DIT_ATTN_ERR_PARTS",
     -11: "DIT_ATTN_ERR_LIMIT",
     -12: "DIT_ATTN_ERR_CAPTURE",
+    -13: "DIT_ATTN_ERR_MASK",
+    -14: "DIT_ATTN_ERR_ROPE",
+    -15: "DIT_ATTN_ERR_NORM",
+    -16: "DIT_ATTN_ERR_STRIDE",
 }
 
 
@@ -70,6 +89,69 @@ class SchedCandidate(ctypes.Structure):
     """dit_sched_candidate of include/dit_sched.h."""
     _fields_ = [("gpus", ctypes.c_int32), ("gpu_mask", ctypes.c_uint32), ("laxity", ctypes.c_double),
                 ("hold", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS = 0, 1, 2, 3
+ROPE_INTERLEAVED, ROPE_HALF = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+
+
+class RopeSpec(ctypes.Structure):
+    """dit_attn_rope of include/dit_attn.h.  axis_dim: rotated elements of each axis; theta, factor and original_length: one
+    value for all axes or one for each."""
+    _fields_ = [("n_axes", ctypes.c_int32), ("scaling", ctypes.c_int32), ("axis_dim", ctypes.c_int32 * 4),
+                ("theta", ctypes.c_double * 4), ("factor", ctypes.c_double * 4), ("original_length", ctypes.c_double * 4),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+    def __init__(self, axis_dim, theta=10000.0, scaling=ROPE_PLAIN, factor=1.0, original_length=0.0, low=1.0, high=32.0,
+                 magnitude=1.0):
+        dims = [int(d) for d in axis_dim]
+
+        def each(name, x):
+            vals = [float(v) for v in x] if hasattr(x, "__len__") else [float(x)] * len(dims)
+            if len(vals) != len(dims):
+                raise ValueError(f"{name}: one value, or one for each of the {len(dims)} axes")
+            return (ctypes.c_double * 4)(*vals)
+
+        if not 1 <= len(dims) <= 4:
+            raise ValueError("1 to 4 axes")
+        super().__init__(len(dims), int(scaling), (ctypes.c_int32 * 4)(*dims), each("theta", theta), each("factor", factor),
+                         each("original_length", original_length), float(low), float(high), float(magnitude))
+
+    @property
+    def rot_dim(self) -> int:
+        return sum(self.axis_dim[:self.n_axes])
+
+
+class NormHeads(ctypes.Structure):
+    """dit_attn_norm_heads of include/dit_attn.h: one side, queries or keys.  x and out: bf16 tensors [n_rows, n_heads, head_dim]
+    whose heads are contiguous (rows may be strided), out = x replaces in place; or integer addresses with n_heads given.
+    weight, bias: fp32 [head_dim] or None."""
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("n_heads", ctypes.c_int32)]
+
+    def __init__(self, x, out, weight=None, bias=None, n_heads=None, row_stride=None, out_row_stride=None):
+        if n_heads is None:
+            n_heads = x.shape[1]
+        super().__init__(_ptr(x), _ptr(out), _row_stride(x, "x") if row_stride is None else int(row_stride),
+                         _row_stride(out, "out") if out_row_stride is None else int(out_row_stride), _ptr(weight), _ptr(bias), int(n_heads))
+        self._held = (x, out, weight, bias)
+
+
+class AttnMask(ctypes.Structure):
+    """dit_attn_mask of include/dit_attn.h.  prefix: host integers, one a sequence; slopes: device fp32 [n_heads]; q_doc, k_doc:
+    device int32 [Tq], [Tk]."""
+    _fields_ = [("causal", ctypes.c_int32), ("softcap", ctypes.c_float), ("prefix", ctypes.POINTER(ctypes.c_int32)),
+                ("slopes", ctypes.c_void_p), ("q_doc", ctypes.c_void_p), ("k_doc", ctypes.c_void_p)]
+
+    def __init__(self, causal=False, prefix=None, softcap=0.0, slopes=None, q_doc=None, k_doc=None):
+        self.n_prefix = None
+        if prefix is not None:
+            prefix = [int(x) for x in prefix]
+            self.n_prefix = len(prefix)
+            prefix = (ctypes.c_int32 * max(len(prefix), 1))(*prefix)
+        super().__init__(int(causal), float(softcap), prefix, _ptr(slopes), _ptr(q_doc), _ptr(k_doc))
+        self._held = (prefix, slopes, q_doc, k_doc)
 
 
 class DitAttnError(RuntimeError):
@@ -110,6 +192,14 @@ def load_library() -> ctypes.CDLL:
     for fn in (lib.dit_attn_sp_pack_heads, lib.dit_attn_sp_unpack_heads):
         fn.restype = ctypes.c_int
         fn.argtypes = [vp, vp, vp, i64, i32, i32, i32, vp]
+    lib.dit_attn_rope_table.restype = ctypes.c_int
+    lib.dit_attn_rope_table.argtypes = [vp, vp, i64, ctypes.POINTER(RopeSpec), vp, vp]
+    lib.dit_attn_qk_norm_rope.restype = ctypes.c_int
+    lib.dit_attn_qk_norm_rope.argtypes = [vp, ctypes.POINTER(NormHeads), ctypes.POINTER(NormHeads), i64, i32, i32, ctypes.c_float, vp,
+                                          i32, i32, vp]
+    lib.dit_attn_masked_varlen_fwd.restype = ctypes.c_int
+    lib.dit_attn_masked_varlen_fwd.argtypes = [vp, vp, vp, vp, ctypes.POINTER(i64), vp, vp, i32, i32, i32, i32, ctypes.c_float,
+                                               ctypes.POINTER(AttnMask), vp, vp, vp]
     lib.dit_sched_laxity.restype = ctypes.c_double
     lib.dit_sched_laxity.argtypes = [ctypes.c_double, ctypes.c_double, i32, ctypes.c_double]
     f64p = ctypes.POINTER(ctypes.c_double)
@@ -142,6 +232,16 @@ def _ptr(x) -> int:
     if hasattr(x, "data_ptr"):
         return int(x.data_ptr())
     return int(x)
+
+
+def _row_stride(x, name: str) -> int:
+    """Elements from row to row of a bf16 tensor [rows, heads, head_dim] with contiguous heads; 0 (contiguous) for an address."""
+    if not hasattr(x, "stride"):
+        return 0
+    shape, (rows, heads, inner) = x.shape, x.stride()
+    if x.element_size() != 2 or (inner != 1 and shape[2] > 1) or (heads != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name}: a bf16 tensor [rows, heads, head_dim] whose heads are contiguous")
+    return rows if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _cu_array(cu_seqlens) -> np.ndarray:
@@ -306,6 +406,47 @@ def dit_attn_sp_pack_heads(ctx, src, dst, n_rows: int, n_heads: int, head_dim: i
 def dit_attn_sp_unpack_heads(ctx, src, dst, n_rows: int, n_heads: int, head_dim: int, sp_degree: int, stream=None) -> None:
     """[p, n_rows, H/p, D] -> [n_rows, H, D] (block g came from rank g); see include/dit_attn.h."""
     _sp_layout("dit_attn_sp_unpack_heads", ctx, src, dst, n_rows, n_heads, head_dim, sp_degree, stream)
+
+
+def dit_attn_rope_table(ctx, positions, n_rows: int, rope: RopeSpec, table, stream=None) -> None:
+    """table[r, pair] = (cos, sin) of the row's positions; positions: device int32 [n_rows, n_axes]; see include/dit_attn.h."""
+    rc = load_library().dit_attn_rope_table(ctx, _ptr(positions), n_rows, rope, _ptr(table), _ptr(stream))
+    if rc != 0:
+        raise DitAttnError(rc, dit_attn_last_error(ctx))
+
+
+def dit_attn_qk_norm_rope(ctx, q, k, n_rows: int, head_dim: int, norm: int, eps: float, table=None, rot_dim: int = 0,
+                          layout: int = ROPE_INTERLEAVED, stream=None) -> None:
+    """Norm of queries and keys for each head and rotation; q, k: NormHeads, or None for one of them; see include/dit_attn.h."""
+    rc = load_library().dit_attn_qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, _ptr(table), rot_dim, layout, _ptr(stream))
+    if rc != 0:
+        raise DitAttnError(rc, dit_attn_last_error(ctx))
+
+
+def dit_attn_masked_varlen_fwd(ctx, q, k, v, cu_seqlens_q, cu_seqlens_k, n_heads: int, n_kv_heads: int, head_dim: int, scale: float,
+                               mask: AttnMask | None, out, lse=None, stream=None, row_strides=None, n_seqs: int | None = None) -> None:
+    """Attention with masks, capped scores and a distance bias; see include/dit_attn.h.
+
+    q, k, v: bf16 tensors [rows, heads, head_dim] whose rows may be strided, or integer addresses (with row_strides, three
+    numbers of elements, unless contiguous).  cu_seqlens_k may be None (that of the queries); mask, lse may be None.
+    """
+    lib = load_library()
+    cq = _cu_array(cu_seqlens_q)
+    ck = None if cu_seqlens_k is None else _cu_array(cu_seqlens_k)
+    if n_seqs is None:
+        n_seqs = len(cq) - 1
+    if (ck is not None and len(ck) <= n_seqs) or len(cq) <= n_seqs:
+        raise ValueError("cu_seqlens_q and cu_seqlens_k need n_seqs + 1 entries")
+    if mask is not None and mask.n_prefix is not None and mask.n_prefix < n_seqs:
+        raise ValueError("mask.prefix needs an entry for every sequence")
+    if row_strides is None and hasattr(q, "stride"):
+        row_strides = (_row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v"))
+    if row_strides is not None:
+        row_strides = (ctypes.c_int64 * 3)(*row_strides)
+    rc = lib.dit_attn_masked_varlen_fwd(ctx, _ptr(q), _ptr(k), _ptr(v), row_strides, cq.ctypes.data, None if ck is None else ck.ctypes.data,
+                                        n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, _ptr(out), _ptr(lse), _ptr(stream))
+    if rc != 0:
+        raise DitAttnError(rc, dit_attn_last_error(ctx))
 
 
 def dit_attn_plan(cu_seqlens, n_heads: int, head_dim: int):

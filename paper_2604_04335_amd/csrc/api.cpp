@@ -15,6 +15,8 @@
 #include <vector>
 
 #include "attn_fwd.h"
+#include "context.h"
+#include "masked_attn.h"
 #include "merge.h"
 #include "noalloc.h"
 #include "plan.h"
@@ -22,93 +24,17 @@
 
 namespace {
 
-struct CachedPlan {
-  std::vector<int32_t> cu;  // key: cu_seqlens contents (of the queries)
-  std::vector<int32_t> cu_k;  // key: key boundaries, empty when they are the query boundaries
-  int32_t n_heads = 0;
-  int32_t head_dim = 0;
-  dit::AttnKernel kernel = dit::AttnKernel::kIndependent128;
-  int32_t n_splits = 1;  // key chunks per sequence (split-KV); part of the key
-  std::vector<dit::WorkItem> host_items;
-  dit::WorkItem* dev_items = nullptr;
-  uint64_t last_use = 0;
-  bool pinned = false;  // a launch that reads dev_items was recorded into a HIP graph: never evicted
-};
-
-constexpr size_t kMaxCachedPlans = 32;
 constexpr int kMi355xComputeUnits = 256;  // what dit_attn_plan assumes when it has no device to ask
 constexpr size_t kMaxItems = size_t(1) << 30;
 
 thread_local std::string g_create_error;
 
-}  // namespace
-
-struct dit_attn_ctx {
-  int device = 0;
-  int n_cus = 0;
-  uint32_t* sync = nullptr;     // device, 8 words: work counters (zero between launches) and the last launch's clock sample
-  uint64_t tick = 0;
-  int force_kernel = -1;        // -1: chosen per pack; else a dit::AttnKernel value (dit_attn_set_kernel)
-  int last_kernel = -1;         // kernel of the last attention launch (dit_attn_last_launch_kernel)
-  int max_splits = 1;           // split-KV: at most this many key chunks per sequence (dit_attn_set_split_kv); 1 = off
-  float* workspace = nullptr;   // split-KV partial results and their lse
-  size_t workspace_bytes = 0;
-  bool workspace_pinned = false;        // a captured graph refers to `workspace`: kept until destroy when it is outgrown
-  std::vector<float*> retired_workspaces;
-  std::vector<std::unique_ptr<CachedPlan>> plans;
-  std::string error;
-};
-
-namespace {
-
-int fail(dit_attn_ctx* ctx, int code, const std::string& msg) {
-  if (ctx) ctx->error = msg;
-  return code;
-}
-
-int fail_hip(dit_attn_ctx* ctx, hipError_t e, const char* what) {
-  // Clear the sticky error so that it is not reported by an unrelated later call.
-  (void)hipGetLastError();
-  return fail(ctx, DIT_ATTN_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
-
-struct DeviceGuard {
-  int prev = -1;
-  bool switched = false;
-  hipError_t enter(int dev) {
-    hipError_t e = hipGetDevice(&prev);
-    if (e != hipSuccess) return e;
-    if (prev != dev) {
-      e = hipSetDevice(dev);
-      if (e != hipSuccess) return e;
-      switched = true;
-    }
-    return hipSuccess;
-  }
-  ~DeviceGuard() {
-    if (switched) (void)hipSetDevice(prev);
-  }
-};
-
-int check_shape_args(const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_heads, int32_t head_dim, std::string& msg) {
-  if (!cu_seqlens) {
-    msg = "cu_seqlens is NULL";
-    return DIT_ATTN_ERR_NULL;
-  }
-  if (head_dim != 64 && head_dim != 128) {
-    msg = "head_dim must be 64 or 128, got " + std::to_string(head_dim);
-    return DIT_ATTN_ERR_HEAD_DIM;
-  }
-  if (n_heads < 1 || n_heads > 65535) {
-    msg = "n_heads must be in 1..65535, got " + std::to_string(n_heads);
-    return DIT_ATTN_ERR_N_HEADS;
-  }
-  if (dit::plan_validate(cu_seqlens, n_seqs) != 0) {
-    msg = "cu_seqlens must start at 0 and be non-decreasing, n_seqs >= 0";
-    return DIT_ATTN_ERR_CU_SEQLENS;
-  }
-  return DIT_ATTN_OK;
-}
+using dit::CachedPlan;
+using dit::check_shape_args;
+using dit::DeviceGuard;
+using dit::fail;
+using dit::fail_hip;
+using dit::kMaxCachedPlans;
 
 }  // namespace
 
@@ -153,6 +79,7 @@ int dit_attn_create(dit_attn_ctx** out_ctx, int device_id) {
   if (e == hipSuccess) e = hipMemset(ctx->sync, 0, 8 * sizeof(uint32_t));
   // Kernel code resident and LDS limits set before the first launch; this device's fixed scratch resolved.
   if (e == hipSuccess) e = dit::attn_fwd_prepare();
+  if (e == hipSuccess) e = dit::masked_attn_prepare();
   if (e == hipSuccess) e = dit::noalloc_init(device_id);
   if (e != hipSuccess) {
     (void)hipGetLastError();
@@ -326,9 +253,7 @@ int forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* v, cons
 
   // A call that is being recorded into a HIP graph may neither allocate nor copy synchronously, and what it records
   // keeps reading the work-list (and the split-KV workspace) on every replay.
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  const bool capturing = hipStreamIsCapturing(s, &cap) == hipSuccess && cap == hipStreamCaptureStatusActive;
-  (void)hipGetLastError();
+  const bool capturing = dit::stream_capturing(s);
 
   // Plan cache: the same pack comes back for every DiT block of every step.
   CachedPlan* plan = nullptr;
@@ -408,23 +333,9 @@ int forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* v, cons
   if (n_splits > 1) {
     const size_t need = static_cast<size_t>(n_splits) * static_cast<size_t>(total_q) * static_cast<size_t>(n_heads) *
                         (static_cast<size_t>(head_dim) + 1) * sizeof(float);
-    if (need > ctx->workspace_bytes) {
-      if (capturing)
-        return fail(ctx, DIT_ATTN_ERR_CAPTURE, "the stream is capturing and the split-KV workspace would have to grow: call once outside the capture first");
-      if (ctx->workspace && ctx->workspace_pinned) {
-        ctx->retired_workspaces.push_back(ctx->workspace);  // a captured graph still writes there on replay
-        ctx->workspace_pinned = false;
-      } else if (ctx->workspace) {
-        (void)hipFree(ctx->workspace);  // waits for the device: no kernel still uses it
-      }
-      ctx->workspace = nullptr;
-      ctx->workspace_bytes = 0;
-      e = hipMalloc(reinterpret_cast<void**>(&ctx->workspace), need);
-      if (e != hipSuccess) return fail_hip(ctx, e, "hipMalloc(split-KV workspace)");
-      ctx->workspace_bytes = need;
-    }
+    rc = dit::ensure_workspace(ctx, need, capturing, "split-KV");
+    if (rc != DIT_ATTN_OK) return rc;
   }
-  if (n_splits > 1 && capturing) ctx->workspace_pinned = true;
   float* part_out = n_splits > 1 ? ctx->workspace : nullptr;
   float* part_lse = n_splits > 1 ? ctx->workspace + static_cast<size_t>(n_splits) * total_q * n_heads * head_dim : nullptr;
   if (n_splits > 1) {

@@ -1,0 +1,320 @@
+// C ABI of the operators around the attention and of attention with masks: argument checks, split of the keys, launch.
+#include "../../include/dit_attn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <numeric>
+#include <string>
+#include <vector>
+
+#include "context.h"
+#include "masked_attn.h"
+#include "qk_norm_rope.h"
+
+namespace {
+
+using dit::fail;
+using dit::fail_hip;
+
+bool misaligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+// No exception leaves a C entry.
+template <class F>
+int guarded(dit_attn_ctx* ctx, F&& body) {
+  if (!ctx) return DIT_ATTN_ERR_NULL;
+  try {
+    ctx->error.clear();
+    return body();
+  } catch (...) {
+    return DIT_ATTN_ERR_HIP;  // out of host memory
+  }
+}
+
+// ---------------------------------------------------------------- rotation table
+
+// Radians per position of pair j of an axis.
+double rope_frequency(const dit_attn_rope& r, int axis, int j) {
+  const double d = r.axis_dim[axis], theta = r.theta[axis], s = r.factor[axis];
+  double f = std::pow(theta, -2.0 * j / d);
+  if (r.scaling == DIT_ATTN_ROPE_LINEAR) return f / s;
+  if (r.scaling == DIT_ATTN_ROPE_BASE && d > 2) return std::pow(theta * std::pow(s, d / (d - 2.0)), -2.0 * j / d);
+  if (r.scaling == DIT_ATTN_ROPE_BANDS) {
+    const double turns = r.original_length[axis] * f / (2.0 * 3.14159265358979323846);
+    const double g = std::min(1.0, std::max(0.0, (turns - r.low) / (r.high - r.low)));
+    return f * (g + (1.0 - g) / s);
+  }
+  return f;
+}
+
+int rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_rows, const dit_attn_rope* r, float* table, void* stream) {
+  if (!r) return fail(ctx, DIT_ATTN_ERR_NULL, "rope is NULL");
+  if (r->n_axes < 1 || r->n_axes > 4) return fail(ctx, DIT_ATTN_ERR_ROPE, "n_axes must be in 1..4");
+  if (r->scaling < DIT_ATTN_ROPE_PLAIN || r->scaling > DIT_ATTN_ROPE_BANDS) return fail(ctx, DIT_ATTN_ERR_ROPE, "no such scaling");
+  if (!std::isfinite(r->magnitude) || std::fabs(r->magnitude) > 1e30) return fail(ctx, DIT_ATTN_ERR_ROPE, "magnitude must be finite");
+  int total = 0;
+  for (int a = 0; a < r->n_axes; ++a) {
+    if (r->axis_dim[a] < 2 || r->axis_dim[a] % 2 != 0 || r->axis_dim[a] > 2 * dit::kMaxRopePairs)
+      return fail(ctx, DIT_ATTN_ERR_ROPE, "axis_dim must be even and in 2..128");
+    total += r->axis_dim[a];
+    if (!(r->theta[a] >= 1.0) || !std::isfinite(r->theta[a])) return fail(ctx, DIT_ATTN_ERR_ROPE, "theta must be finite and at least 1");
+    if (r->scaling != DIT_ATTN_ROPE_PLAIN && (!(r->factor[a] >= 1.0) || !std::isfinite(r->factor[a])))
+      return fail(ctx, DIT_ATTN_ERR_ROPE, "factor must be finite and at least 1");
+    if (r->scaling == DIT_ATTN_ROPE_BANDS && (!(r->original_length[a] > 0.0) || !std::isfinite(r->original_length[a])))
+      return fail(ctx, DIT_ATTN_ERR_ROPE, "original_length must be positive");
+  }
+  if (total > 2 * dit::kMaxRopePairs) return fail(ctx, DIT_ATTN_ERR_ROPE, "the axes have more than 128 elements together");
+  if (r->scaling == DIT_ATTN_ROPE_BANDS && !(r->low < r->high && std::isfinite(r->low) && std::isfinite(r->high)))
+    return fail(ctx, DIT_ATTN_ERR_ROPE, "low must be under high");
+  if (n_rows < 0) return fail(ctx, DIT_ATTN_ERR_CU_SEQLENS, "n_rows must be >= 0");
+  if (n_rows == 0) return DIT_ATTN_OK;
+  if (!positions || !table) return fail(ctx, DIT_ATTN_ERR_NULL, "positions and table must be non-NULL");
+  if (misaligned(positions, 4) || misaligned(table, 16))
+    return fail(ctx, DIT_ATTN_ERR_ALIGN, "positions must be 4-byte, table 16-byte aligned");
+  if (n_rows > (int64_t{1} << 34)) return fail(ctx, DIT_ATTN_ERR_LIMIT, "too many rows");
+
+  dit::RopeTableParams p{};
+  p.positions = positions;
+  p.table = table;
+  p.n_rows = n_rows;
+  p.n_axes = r->n_axes;
+  p.n_pairs = total / 2;
+  p.magnitude = static_cast<float>(r->magnitude);
+  int pair = 0;
+  for (int a = 0; a < r->n_axes; ++a)
+    for (int j = 0; j < r->axis_dim[a] / 2; ++j, ++pair) {
+      const long double turns = static_cast<long double>(rope_frequency(*r, a, j)) / 6.283185307179586476925286766559L;
+      p.turns_hi[pair] = static_cast<double>(turns);
+      p.turns_lo[pair] = static_cast<double>(turns - static_cast<long double>(p.turns_hi[pair]));
+      p.axis[pair] = static_cast<uint8_t>(a);
+    }
+  dit::DeviceGuard guard;
+  hipError_t e = guard.enter(ctx->device);
+  if (e != hipSuccess) return fail_hip(ctx, e, "hipSetDevice");
+  e = dit::rope_table_launch(p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DIT_ATTN_OK : fail_hip(ctx, e, "rotation table kernel launch");
+}
+
+// ---------------------------------------------------------------- norm and rotation
+
+int check_norm_heads(dit_attn_ctx* ctx, const dit_attn_norm_heads& s, const char* name, int64_t n_rows, int32_t head_dim, int32_t norm,
+                     dit::NormHeadsParams& out) {
+  const std::string who = std::string(name) + ": ";
+  if (s.n_heads < 1 || s.n_heads > 65535) return fail(ctx, DIT_ATTN_ERR_N_HEADS, who + "n_heads must be in 1..65535");
+  const int64_t row = static_cast<int64_t>(s.n_heads) * head_dim;
+  const int64_t in_stride = s.row_stride ? s.row_stride : row, out_stride = s.out_row_stride ? s.out_row_stride : row;
+  for (const int64_t st : {in_stride, out_stride})
+    if (st < row || st % 8 != 0 || st > (int64_t{1} << 40))
+      return fail(ctx, DIT_ATTN_ERR_STRIDE, who + "row strides must be multiples of 8 elements and hold n_heads * head_dim");
+  if (norm == DIT_ATTN_NORM_NONE && (s.weight || s.bias)) return fail(ctx, DIT_ATTN_ERR_NORM, who + "weight and bias belong to a norm");
+  if (n_rows == 0) return DIT_ATTN_OK;
+  if (!s.x || !s.out) return fail(ctx, DIT_ATTN_ERR_NULL, who + "x and out must be non-NULL");
+  if (misaligned(s.x, 16) || misaligned(s.out, 16) || misaligned(s.weight, 16) || misaligned(s.bias, 16))
+    return fail(ctx, DIT_ATTN_ERR_ALIGN, who + "x, out, weight and bias must be 16-byte aligned");
+  if (s.x == s.out && in_stride != out_stride) return fail(ctx, DIT_ATTN_ERR_STRIDE, who + "in place, both row strides must be equal");
+  out.x = static_cast<const char*>(s.x);
+  out.out = static_cast<char*>(s.out);
+  out.row_stride_b = 2 * in_stride;
+  out.out_stride_b = 2 * out_stride;
+  out.weight = s.weight;
+  out.bias = s.bias;
+  out.n_heads = s.n_heads;
+  return DIT_ATTN_OK;
+}
+
+int qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const dit_attn_norm_heads* k, int64_t n_rows, int32_t head_dim,
+                 int32_t norm, float eps, const float* table, int32_t rot_dim, int32_t layout, void* stream) {
+  if (!q && !k) return fail(ctx, DIT_ATTN_ERR_NULL, "q and k are both NULL");
+  if (head_dim != 64 && head_dim != 128) return fail(ctx, DIT_ATTN_ERR_HEAD_DIM, "head_dim must be 64 or 128");
+  if (norm < DIT_ATTN_NORM_NONE || norm > DIT_ATTN_NORM_LAYER) return fail(ctx, DIT_ATTN_ERR_NORM, "no such norm");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(ctx, DIT_ATTN_ERR_NORM, "eps must be finite and not negative");
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 8 != 0)
+    return fail(ctx, DIT_ATTN_ERR_ROPE, "rot_dim must be a multiple of 8 in 0..head_dim");
+  if (layout != DIT_ATTN_ROPE_INTERLEAVED && layout != DIT_ATTN_ROPE_HALF) return fail(ctx, DIT_ATTN_ERR_ROPE, "no such layout");
+  if (n_rows < 0) return fail(ctx, DIT_ATTN_ERR_CU_SEQLENS, "n_rows must be >= 0");
+  dit::QkNormRopeParams p{};
+  if (q) {
+    const int rc = check_norm_heads(ctx, *q, "q", n_rows, head_dim, norm, p.side[0]);
+    if (rc != DIT_ATTN_OK) return rc;
+  }
+  if (k) {
+    const int rc = check_norm_heads(ctx, *k, "k", n_rows, head_dim, norm, p.side[1]);
+    if (rc != DIT_ATTN_OK) return rc;
+  }
+  if (n_rows == 0) return DIT_ATTN_OK;
+  if (rot_dim > 0 && !table) return fail(ctx, DIT_ATTN_ERR_NULL, "table is NULL");
+  if (rot_dim > 0 && misaligned(table, 16)) return fail(ctx, DIT_ATTN_ERR_ALIGN, "table must be 16-byte aligned");
+  p.table = table;
+  p.n_rows = n_rows;
+  p.rot_dim = rot_dim;
+  p.half = layout == DIT_ATTN_ROPE_HALF ? 1 : 0;
+  p.eps = eps;
+  if (n_rows > (int64_t{1} << 34) || dit::qk_norm_rope_blocks(p, head_dim) > 0x7FFFFFFF)
+    return fail(ctx, DIT_ATTN_ERR_LIMIT, "too many rows");
+  dit::DeviceGuard guard;
+  hipError_t e = guard.enter(ctx->device);
+  if (e != hipSuccess) return fail_hip(ctx, e, "hipSetDevice");
+  e = dit::qk_norm_rope_launch(p, static_cast<dit::HeadNorm>(norm), head_dim, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DIT_ATTN_OK : fail_hip(ctx, e, "norm and rotation kernel launch");
+}
+
+// ---------------------------------------------------------------- masked attention
+
+int64_t tiles_of(int64_t keys) { return (keys + 63) / 64; }
+
+// Parts that the keys of every sequence are split into, and the tiles of a part.
+// Few rows: a workgroup (160 KB of LDS, so one on a compute unit) for each of them, at least four tiles each.
+// Else: where the items leave half of the workgroups' places idle, parts of at least sixteen tiles.
+void choose_parts(int64_t items, int64_t max_tiles, bool few_rows, int n_cus, int32_t* n_parts, int32_t* part_tiles) {
+  const int64_t places = few_rows ? n_cus : 2 * static_cast<int64_t>(n_cus);
+  int64_t n = std::min<int64_t>({places / std::max<int64_t>(items, 1), max_tiles / (few_rows ? 4 : 16), dit::kMaskedMaxParts});
+  n = std::max<int64_t>(n, 1);
+  const int64_t per = std::max<int64_t>((max_tiles + n - 1) / n, 1);
+  *part_tiles = static_cast<int32_t>(per);
+  *n_parts = static_cast<int32_t>(std::max<int64_t>((max_tiles + per - 1) / per, 1));
+}
+
+int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* v, const int64_t* row_strides, const int32_t* cu_q,
+                   const int32_t* cu_k, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                   const dit_attn_mask* mask, void* out, float* lse, void* stream) {
+  std::string msg;
+  int rc = dit::check_shape_args(cu_q, n_seqs, n_heads, head_dim, msg);
+  if (rc != DIT_ATTN_OK) return fail(ctx, rc, msg);
+  if (cu_k && dit::plan_validate(cu_k, n_seqs) != 0)
+    return fail(ctx, DIT_ATTN_ERR_CU_SEQLENS, "cu_seqlens_k must start at 0 and be non-decreasing");
+  if (!cu_k) cu_k = cu_q;
+  if (n_kv_heads < 1 || n_heads % n_kv_heads != 0) return fail(ctx, DIT_ATTN_ERR_N_HEADS, "n_kv_heads must be >= 1 and divide n_heads");
+  if (!std::isfinite(scale)) return fail(ctx, DIT_ATTN_ERR_SCALE, "scale must be finite");
+  const dit_attn_mask no_mask{};
+  const dit_attn_mask& m = mask ? *mask : no_mask;
+  if (m.causal != 0 && m.causal != 1) return fail(ctx, DIT_ATTN_ERR_MASK, "causal must be 0 or 1");
+  if (!(m.softcap >= 0.f) || !std::isfinite(m.softcap)) return fail(ctx, DIT_ATTN_ERR_MASK, "softcap must be finite and not negative");
+  if (m.prefix && !m.causal) return fail(ctx, DIT_ATTN_ERR_MASK, "prefix belongs to a causal mask");
+  if (m.prefix)
+    for (int32_t i = 0; i < n_seqs; ++i)
+      if (m.prefix[i] < 0) return fail(ctx, DIT_ATTN_ERR_MASK, "prefix must not be negative");
+  if ((m.q_doc == nullptr) != (m.k_doc == nullptr)) return fail(ctx, DIT_ATTN_ERR_MASK, "q_doc and k_doc come together");
+  const int64_t dense[3] = {static_cast<int64_t>(n_heads) * head_dim, static_cast<int64_t>(n_kv_heads) * head_dim,
+                            static_cast<int64_t>(n_kv_heads) * head_dim};
+  const int64_t* strides = row_strides ? row_strides : dense;
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < dense[i] || strides[i] % 8 != 0 || strides[i] > (int64_t{1} << 24))
+      return fail(ctx, DIT_ATTN_ERR_STRIDE, "row strides must be multiples of 8 elements, hold a row's heads and be at most 2^24");
+  const int64_t total_q = n_seqs > 0 ? cu_q[n_seqs] : 0, total_k = n_seqs > 0 ? cu_k[n_seqs] : 0;
+  if (total_q == 0) return DIT_ATTN_OK;
+  if (!q || !out || (total_k > 0 && (!k || !v))) return fail(ctx, DIT_ATTN_ERR_NULL, "q, k, v and out must be non-NULL");
+  if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16))
+    return fail(ctx, DIT_ATTN_ERR_ALIGN, "q, k, v and out must be 16-byte aligned");
+  if (misaligned(lse, 4) || misaligned(m.slopes, 4) || misaligned(m.q_doc, 4) || misaligned(m.k_doc, 4))
+    return fail(ctx, DIT_ATTN_ERR_ALIGN, "lse, slopes, q_doc and k_doc must be 4-byte aligned");
+
+  // Sequences with query rows, the most keys first: their items take longest.
+  std::vector<int32_t> order;
+  int64_t max_rows = 0, items = 0, max_tiles = 0, total_tiles = 0;
+  const int32_t group = n_heads / n_kv_heads;
+  for (int32_t i = 0; i < n_seqs; ++i) {
+    const int64_t lq = cu_q[i + 1] - cu_q[i], lk = cu_k[i + 1] - cu_k[i];
+    if (lq == 0) continue;
+    order.push_back(i);
+    max_rows = std::max(max_rows, lq);
+    max_tiles = std::max(max_tiles, tiles_of(lk));
+    total_tiles += tiles_of(lk);
+    items += (lq + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads;
+  }
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cu_k[a + 1] - cu_k[a] > cu_k[b + 1] - cu_k[b]; });
+  const bool few_rows = max_rows * group <= dit::kMaskedFewRows;
+  if (few_rows) items = static_cast<int64_t>(order.size()) * n_kv_heads;
+
+  dit::MaskedParams p{};
+  choose_parts(items, max_tiles, few_rows, ctx->n_cus, &p.n_parts, &p.part_tiles);
+  if (items * p.n_parts > 0x7FFFFFFF) return fail(ctx, DIT_ATTN_ERR_LIMIT, "pack has too many work items");
+
+  dit::DeviceGuard guard;
+  hipError_t e = guard.enter(ctx->device);
+  if (e != hipSuccess) return fail_hip(ctx, e, "hipSetDevice");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+
+  const bool docs = m.q_doc != nullptr;
+  const size_t doc_bytes = docs ? (static_cast<size_t>(total_tiles) * sizeof(dit::DocTile) + 255) / 256 * 256 : 0;
+  const size_t part_rh = p.n_parts > 1 ? static_cast<size_t>(p.n_parts) * static_cast<size_t>(total_q) * static_cast<size_t>(n_heads) : 0;
+  const size_t need = doc_bytes + part_rh * (static_cast<size_t>(head_dim) + 1) * sizeof(float);
+  if (need > 0) {
+    rc = dit::ensure_workspace(ctx, need, dit::stream_capturing(s), "masked attention");
+    if (rc != DIT_ATTN_OK) return rc;
+    if (docs) p.doc_tiles = reinterpret_cast<dit::DocTile*>(ctx->workspace);
+    if (p.n_parts > 1) {
+      p.part_out = ctx->workspace + doc_bytes / sizeof(float);
+      p.part_lse = p.part_out + part_rh * head_dim;
+    }
+  }
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.out = out;
+  p.lse = lse;
+  p.part_rows = total_q;
+  p.n_heads = n_heads;
+  p.group = group;
+  p.c_true = std::fabs(scale) * 1.44269504088896340736f;
+  p.c_log2 = std::max(p.c_true, 1e-30f);
+  p.negate = scale < 0.f ? 1 : 0;
+  if (m.softcap > 0.f) {
+    p.tanh_in = static_cast<float>(2.0 * 1.44269504088896340736 * std::fabs(static_cast<double>(scale)) / m.softcap);
+    p.cap_log2 = m.softcap * 1.44269504088896340736f;
+  }
+  p.q_stride_b = 2 * strides[0];
+  p.k_stride_b = 2 * strides[1];
+  p.v_stride_b = 2 * strides[2];
+  p.q_doc = m.q_doc;
+  p.k_doc = m.k_doc;
+  p.slopes = m.slopes;
+  p.causal = m.causal;
+  const dit::MaskedKind kind = {head_dim, few_rows, m.softcap > 0.f, m.slopes != nullptr, lse != nullptr || p.n_parts > 1};
+  for (size_t first = 0; first < order.size(); first += dit::kMaskedSeqs) {
+    p.n = static_cast<int32_t>(std::min<size_t>(order.size() - first, dit::kMaskedSeqs));
+    uint32_t item = 0, tile = 0;
+    for (int32_t i = 0; i < p.n; ++i) {
+      const int32_t sq = order[first + static_cast<size_t>(i)];
+      dit::MaskedSeq& d = p.seq[i];
+      d = {item, tile, cu_q[sq], cu_q[sq + 1] - cu_q[sq], cu_k[sq], cu_k[sq + 1] - cu_k[sq], m.prefix ? m.prefix[sq] : 0};
+      const int64_t blocks = few_rows ? n_kv_heads : (static_cast<int64_t>(d.q_len) + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads;
+      item += static_cast<uint32_t>(blocks * p.n_parts);
+      tile += static_cast<uint32_t>(tiles_of(d.kv_len));
+    }
+    p.n_items = item;
+    e = dit::masked_attn_launch(p, kind, docs ? tile : 0, s);
+    if (e != hipSuccess) return fail_hip(ctx, e, "masked attention kernel launch");
+  }
+  if (p.n_parts > 1) {
+    e = dit::masked_join_launch(p, head_dim, s);
+    if (e != hipSuccess) return fail_hip(ctx, e, "join kernel launch");
+  }
+  return DIT_ATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dit_attn_rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_rows, const dit_attn_rope* rope, float* table, void* stream) {
+  return guarded(ctx, [&] { return rope_table(ctx, positions, n_rows, rope, table, stream); });
+}
+
+int dit_attn_qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const dit_attn_norm_heads* k, int64_t n_rows, int32_t head_dim,
+                          int32_t norm, float eps, const float* table, int32_t rot_dim, int32_t layout, void* stream) {
+  return guarded(ctx, [&] { return qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, table, rot_dim, layout, stream); });
+}
+
+int dit_attn_masked_varlen_fwd(dit_attn_ctx* ctx, const void* q, const void* k, const void* v, const int64_t* row_strides,
+                               const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int32_t n_seqs, int32_t n_heads,
+                               int32_t n_kv_heads, int32_t head_dim, float scale, const dit_attn_mask* mask, void* out, float* lse,
+                               void* stream) {
+  return guarded(ctx, [&] {
+    return masked_forward(ctx, q, k, v, row_strides, cu_seqlens_q, cu_seqlens_k, n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, out,
+                          lse, stream);
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,56 @@
+// Launch interface of masked attention.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_fwd.h"
+
+namespace dit {
+
+// The sequences travel with the kernel: at most this many a launch, further ones in further launches.
+constexpr int kMaskedSeqs = 64;
+constexpr int kMaskedBlockM = 128;   // query rows of an item
+constexpr int kMaskedFewRows = 32;   // (row, head of a group) columns of an item of the few-rows kernel
+constexpr int kMaskedMaxParts = 64;  // parts that the keys of a sequence are split into
+
+struct MaskedSeq {
+  uint32_t first;  // index of the sequence's first item in the launch
+  uint32_t tile0;  // its first 64-key tile in doc_tiles
+  int32_t q_start, q_len, kv_start, kv_len, prefix;
+};
+
+// Ids of a 64-key tile: the smallest and largest that are documents (hi < lo: none), and the smallest of all.
+struct DocTile {
+  int32_t lo, hi, any_lo, unused;
+};
+
+// The fields of AttnParams: c_log2, negate, q, k, v, out, lse, n_items, n_heads; with parts also part_out, part_lse, part_rows.
+struct MaskedParams : AttnParams {
+  int64_t q_stride_b, k_stride_b, v_stride_b;  // bytes from row to row
+  const int32_t* q_doc;    // [Tq] or nullptr
+  const int32_t* k_doc;    // [Tk]
+  DocTile* doc_tiles;
+  const float* slopes;     // [n_heads] or nullptr
+  float c_true;            // |scale| * log2(e)
+  float tanh_in;           // 2 * log2(e) * |scale| / cap
+  float cap_log2;          // cap * log2(e)
+  int32_t causal;
+  int32_t group;           // query heads per key head
+  int32_t n_parts;         // parts per sequence
+  int32_t part_tiles;      // 64-key tiles of a part
+  int32_t n;               // sequences
+  MaskedSeq seq[kMaskedSeqs];
+};
+
+struct MaskedKind {
+  int head_dim;
+  bool few_rows, cap, bias, lse;
+};
+
+hipError_t masked_attn_prepare();
+// Doc tiles of the launch's sequences, then the attention kernel on p.n_items workgroups.
+hipError_t masked_attn_launch(const MaskedParams& p, const MaskedKind& kind, uint32_t n_doc_tiles, hipStream_t stream);
+// out, lse (or nullptr) from n_parts partial results of n_rows rows.
+hipError_t masked_join_launch(const MaskedParams& p, int head_dim, hipStream_t stream);
+
+}  // namespace dit

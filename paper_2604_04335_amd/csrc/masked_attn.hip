@@ -1,0 +1,824 @@
+// Attention with masks, capped scores and a distance bias for gfx950 (MI355X).  The tile code is that of the unmasked kernels
+// (attn_device.h): 32 query rows a wavefront, S^T = K Q^T and O^T += V^T P^T on the 32x32x16 bf16 MFMA, 64 keys a tile.
+//
+//   s = scale <q, k>;  with a cap  C tanh(s / C);  with slopes  s - slope_h |pos - j|,  pos = row + keys - rows of the sequence
+//   key j is seen by a row  iff  (not causal or j <= pos or j < prefix) and (no ids or the ids agree and are not negative)
+//   O = sum over seen keys exp(s - lse) v,  lse = ln sum exp(s);  a row that sees nothing gets 0 and -inf.
+//
+// A row's causal and prefix mask is one bound: keys under max(pos + 1, prefix).  Tiles that no row of an item sees are not
+// loaded (for document ids a small kernel takes the range of every tile first); tiles that every row sees wholly are not
+// masked; in the others a dead score becomes -inf, one interval test per score plus one comparison of ids.
+//
+// What a row does not see may hold anything.  Scores are replaced, not added to, so a NaN key has no effect; a probability of
+// 0 times a NaN or infinite value would be NaN, so the values of a masked tile are made finite in LDS (each wavefront looks at
+// the rows that it loaded itself), and an item one of whose rows does see such a value adds it behind the loop.
+//
+// Two sums of a row: of the probabilities as rounded for the second contraction, which O is divided by (a convex combination
+// of values whatever the rounding did), and of the fp32 ones, which the log-sum-exp is taken of.
+#include "attn_device.h"
+#include "masked_attn.h"
+
+namespace dit {
+
+constexpr float kLn2 = 0.69314718055994530942f;
+[[maybe_unused]] constexpr float kNoReference = -1.0e30f;  // of a row that has seen no key
+
+__device__ __forceinline__ const MaskedSeq& find_seq(const MaskedParams& p, uint32_t idx, bool tiles) {
+  int j = 0;
+  if (p.n > 1) {
+    static_assert(kMaskedSeqs == 64, "a lane for each sequence");
+    const int lane = threadIdx.x & 63, i = lane < p.n ? lane : 0;
+    j = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < p.n && (tiles ? p.seq[i].tile0 : p.seq[i].first) <= idx));
+  }
+  return p.seq[__builtin_amdgcn_readfirstlane(j)];
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const int y = __shfl_xor(x, d);
+    x = y < x ? y : x;
+  }
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max(int x) { return ~wave_min(~x); }
+
+// Ids of n consecutive places from ids, one a lane (n at most 64 counts).
+__device__ __forceinline__ DocTile doc_range(const int32_t* ids, int n) {
+  const int lane = threadIdx.x & 63;
+  const int id = ids[lane < n ? lane : 0];
+  DocTile r;
+  r.any_lo = wave_min(id);
+  r.lo = wave_min(id < 0 ? INT32_MAX : id);
+  r.hi = wave_max(id < 0 ? -1 : id);
+  r.unused = 0;
+  return r;
+}
+
+__global__ void __launch_bounds__(256) masked_doc_tiles_kernel(MaskedParams p, uint32_t n_tiles) {
+  const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= n_tiles) return;
+  const MaskedSeq& s = find_seq(p, tile, true);
+  const int key0 = (int)(tile - s.tile0) * 64;
+  const DocTile r = doc_range(p.k_doc + s.kv_start + key0, s.kv_len - key0);
+  if ((threadIdx.x & 63) == 0) p.doc_tiles[tile] = r;
+}
+
+// The tiles [.., end) of a part that any row of an item sees, in order: 64 at a time from their id ranges, or simply all.
+struct LiveTiles {
+  const DocTile* ranges;  // of the sequence, or nullptr
+  DocTile mine;           // ids of the item's rows
+  int end, base;
+  uint64_t live, pure;    // of base .. base + 63; pure: all rows and keys have the same document
+
+  __device__ __forceinline__ void look(int t) {
+    base = t;
+    const int i = t + (int)(threadIdx.x & 63);
+    const DocTile r = ranges[i < end ? i : end - 1];
+    live = __builtin_amdgcn_ballot_w64(i < end && r.lo <= mine.hi && r.hi >= mine.lo);
+    pure = __builtin_amdgcn_ballot_w64(r.any_lo == r.hi && mine.any_lo == r.hi && mine.hi == r.hi);
+  }
+  // The first live tile from t on, or end.
+  __device__ __forceinline__ int next(int t) {
+    if (ranges == nullptr) return t < end ? t : end;
+    while (t < end) {
+      if (t >= base + 64) look(t);
+      const uint64_t rest = live >> (t - base);
+      if (rest != 0) return t + __builtin_ctzll(rest);
+      t = base + 64;
+    }
+    return end;
+  }
+  __device__ __forceinline__ bool is_pure(int t) const { return ranges == nullptr || ((pure >> (t - base)) & 1) != 0; }
+};
+
+// Scores of a lane: element i of block kb is key 32 kb + 8 (i / 4) + (i % 4) + 4 hh of the tile.
+__device__ __forceinline__ constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i >> 2) + (i & 3); }
+
+// Raw scores -> base-2 exponents, with the cap and the bias.  at: pos - first key of the tile - 4 hh of this lane.
+template <int NKB, bool CAP, bool BIAS>
+__device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParams& p, float slope_log2, int at) {
+  const float base = (float)at;
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x = s[kb][i];
+      if constexpr (CAP) {
+        // tanh y = 1 - 2 / (exp(2 y) + 1), whose limits need no clamp
+        const float e = __builtin_amdgcn_exp2f(x * p.tanh_in);
+        x = __builtin_fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
+      } else {
+        x *= p.c_true;
+      }
+      if constexpr (BIAS) x = __builtin_fmaf(-slope_log2, __builtin_fabsf(base - (float)key_of(kb, i)), x);
+      s[kb][i] = x;
+    }
+}
+
+// What a lane's row sees of a tile: keys lo <= key < hi of it, less 4 hh, whose ids are `doc` if there are ids.
+struct LaneMask {
+  int lo;
+  unsigned n;
+  __device__ __forceinline__ bool dead(int kb, int i) const { return (unsigned)(key_of(kb, i) - lo) >= n; }
+};
+
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
+typedef __attribute__((address_space(3))) uint32_t lds_u32;
+
+// Dead scores := -inf.  docs: LDS byte of the tile's ids (0 with no ids), hh as everywhere.  With bad != 0 (bits: keys with a
+// value that is not finite) returns whether this lane's row sees one of them.
+template <int NKB>
+__device__ __forceinline__ bool mask_scores(f32x16 (&s)[NKB], LaneMask m, bool have_docs, uint32_t docs, int doc, int hh, uint64_t bad) {
+  bool sees_bad = false;
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      i32x4 id = {doc, doc, doc, doc};
+      if (have_docs) id = *(lds_i32x4*)(uintptr_t)(docs + (uint32_t)(32 * kb + 8 * g + 4 * hh) * 4u);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * g + j;
+        const bool dead = m.dead(kb, i) || id[j] != doc;
+        s[kb][i] = dead ? -__builtin_inff() : s[kb][i];
+        if (bad != 0) sees_bad |= !dead && ((bad >> (key_of(kb, i) + 4 * hh)) & 1) != 0;
+      }
+    }
+  return sees_bad;
+}
+
+// State of a lane's row.
+struct RowState {
+  float m_ref;  // reference of the exponent, see tile_softmax
+  float l;      // sum of the rounded probabilities (this half-wave's keys)
+  float lx;     // sum of the fp32 ones
+};
+
+// Online softmax of one tile, as tile_softmax in attn_device.h, with the fp32 sum and for rows that may have seen nothing yet.
+template <int NKB, int NDB, bool LSE>
+__device__ __forceinline__ void masked_softmax(f32x16 (&s)[NKB], float mx, float c, uint32_t (&pb)[NKB][8], f32x16 (&o)[NDB], RowState& r) {
+  const bool grow = (mx - r.m_ref) * c > kRescaleLog2;
+  if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+    const float m_new = grow ? mx : r.m_ref;
+    const float alpha = __builtin_amdgcn_exp2f((r.m_ref - m_new) * c);
+    r.m_ref = m_new;
+    r.l *= alpha;
+    if constexpr (LSE) r.lx *= alpha;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+  }
+  const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);  // finite, so that a dead score gives 0 in a row without a reference
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+#pragma unroll
+      for (int i = 8 * g; i < 8 * g + 8; i += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], c, -mc));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i + 1], c, -mc));
+        if constexpr (LSE) r.lx += p0 + p1;
+        pb[kb][i >> 1] = pack_bf16x2(p0, p1);
+      }
+      SCHED_FENCE();
+    }
+}
+
+__device__ __forceinline__ bool pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// Values that are not finite of V rows in LDS become 0: N chunks of 16 bytes a lane, `step` apart from `addr`.  Returns the mask
+// of the chunks that held one.
+template <int N>
+__device__ __forceinline__ uint32_t make_finite(uint32_t addr, uint32_t step) {
+  uint32_t found = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    lds_u32x4* at = (lds_u32x4*)(uintptr_t)(addr + i * step);
+    u32x4 w = *at;
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) bad |= pair_not_finite(w[k]);
+    if (bad) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if ((w[k] & 0x7F80u) == 0x7F80u) w[k] &= 0xFFFF0000u;
+        if ((w[k] & 0x7F800000u) == 0x7F800000u) w[k] &= 0xFFFFu;
+      }
+      *at = w;
+      found |= 1u << i;
+    }
+  }
+  return found;
+}
+
+// Behind the loop of an item some of whose rows see a value that is not finite in a masked tile: such values of keys
+// [key0, key1), key stride `step` in blocks of `run`, are added to the rows that see them.  Slow, and seldom.
+template <class T>
+__device__ __forceinline__ void add_not_finite(const MaskedParams& p, const char* vbase, const int32_t* kdoc, int key0, int key1, int run,
+                                               int step, int klim, int doc, int hh, f32x16 (&o)[T::NDB]) {
+  for (int b = key0; b < key1; b += step)
+    for (int j = b; j < b + run && j < key1; ++j) {
+      const uint32_t* row = reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * p.v_stride_b);
+      const int lane = threadIdx.x & 63;
+      const bool bad = pair_not_finite(row[lane & (T::D / 2 - 1)]);
+      if (__builtin_amdgcn_ballot_w64(bad) == 0) continue;
+      const bool seen = j < klim && (kdoc == nullptr || kdoc[j] == doc);
+#pragma unroll
+      for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int d = 32 * db + 8 * (i >> 2) + (i & 3) + 4 * hh;
+          const uint32_t w = row[d >> 1], bits = d & 1 ? w & 0xFFFF0000u : w << 16;
+          if (seen && (bits & 0x7F800000u) == 0x7F800000u) o[db][i] += __builtin_bit_cast(float, bits);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Items of 128 query rows: 4 wavefronts, K and V tiles double buffered, loaded by all.
+// ---------------------------------------------------------------------------------------------
+template <class T>
+constexpr int kDocsOff = T::ITEM_OFF + 16;
+template <class T>
+constexpr int kBadOff = kDocsOff<T> + 2 * T::BN * 4;
+template <class T>
+constexpr int kMaskedLds = kBadOff<T> + 3 * 8;
+
+// 64 ids -> LDS by one direct load of a dword a lane.
+__device__ __forceinline__ void lds_dma_4(const int32_t* base, uint32_t voff, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
+}
+
+// The rows of a wavefront, O^T / l, leave through LDS as whole rows (see store_out in attn_device.h): bf16 to out, or fp32 halves
+// of rows to the workspace.  inv: 1 / l of the lane's row.
+template <class T>
+__device__ __forceinline__ void store_rows(const MaskedParams& p, const Lane<T>& L, const ItemU& it, const f32x16 (&o)[T::NDB], float inv,
+                                           uint32_t stage) {
+  typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+  if (p.part_out != nullptr) {
+    constexpr int CH = T::D / 8, RPS = 64 / CH;  // 16-byte chunks of half a row; half rows per store
+    const int ch = L.lane & (CH - 1), r0 = L.lane / CH, row0 = L.wave * 32 + r0, n_valid = it.q_rows - row0;
+    float* const dst = p.part_out + ((((int64_t)it.part * p.part_rows + it.q_start + row0) * p.n_heads) + it.head) * T::D + ch * 4;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int b = 0; b < T::NDB / 2; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int db = half * (T::NDB / 2) + b;
+          const f32x4 f = {o[db][4 * g + 0] * inv, o[db][4 * g + 1] * inv, o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv};
+          *(lds_u32x4*)(uintptr_t)(stage + (uint32_t)(L.l32 * (CH * 16) + (((8 * b + 2 * g + L.hh) ^ (L.l32 & (CH - 1))) * 16))) =
+              __builtin_bit_cast(u32x4, f);
+        }
+      asm volatile("" ::: "memory");  // LDS serves a wavefront's instructions in order
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < 32 / RPS; ++i) {
+        const int r = r0 + i * RPS;
+        const u32x4 w = *(lds_u32x4*)(uintptr_t)(stage + (uint32_t)(r * (CH * 16) + ((ch ^ (r & (CH - 1))) * 16)));
+        if (i * RPS < n_valid)
+          store_through(reinterpret_cast<u32x4*>(dst + (int64_t)(i * RPS) * p.n_heads * T::D + half * (T::D / 2)), w);
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
+  constexpr int CH = T::ROW_B / 16, RPS = 64 / CH;
+  const uint32_t wr = stage + (uint32_t)(L.l32 * T::ROW_B + L.hh * 8), wsw = (uint32_t)(L.l32 & (CH - 1)) * 16u;
+#pragma unroll
+  for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const u32x2 w = {pack_bf16x2(o[db][4 * g + 0] * inv, o[db][4 * g + 1] * inv), pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
+      *(lds_u32x2*)(uintptr_t)(wr + ((uint32_t)((4 * db + g) * 16) ^ wsw)) = w;
+    }
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+  const int ch = L.lane & (CH - 1), r0 = L.lane / CH, row0 = L.wave * 32 + r0, n_valid = it.q_rows - row0;
+  const int64_t row_b = (int64_t)p.n_heads * T::ROW_B;
+  char* const dst = static_cast<char*>(p.out) + (int64_t)(it.q_start + row0) * row_b + (int64_t)it.head * T::ROW_B + ch * 16;
+#pragma unroll
+  for (int i = 0; i < 32 / RPS; ++i) {
+    const int r = r0 + i * RPS;
+    const u32x4 w = *(lds_u32x4*)(uintptr_t)(stage + (uint32_t)(r * T::ROW_B + ((ch ^ (r & (CH - 1))) * 16)));
+    if (i * RPS < n_valid) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(dst + (int64_t)(i * RPS) * row_b));
+  }
+}
+
+template <class T, bool CAP, bool BIAS, bool LSE>
+__global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu_waves_per_eu(2, 2))) masked_attn_kernel(MaskedParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+  lds_char* smem = (lds_char*)smem_generic;
+  const uint32_t lds = (uint32_t)(uintptr_t)smem;
+  const int tid = threadIdx.x;
+  Lane<T> L;
+  L.init(tid, p.k_stride_b);
+  const uint32_t vvoff = (uint32_t)L.lrow * (uint32_t)p.v_stride_b + (uint32_t)L.vcol;
+
+  // The item: heads fastest, so that with a multiple of eight heads an XCD keeps to its own ones; the last query tiles first,
+  // which see the most keys under a causal mask.
+  const MaskedSeq& sq = find_seq(p, blockIdx.x, false);
+  const int n_heads = p.n_heads, lq = sq.q_len, lk = sq.kv_len;
+  uint32_t local = blockIdx.x - sq.first;
+  ItemU it;
+  it.part = (int)(local % (uint32_t)p.n_parts);
+  local /= (uint32_t)p.n_parts;
+  it.head = (int)(local % (uint32_t)n_heads);
+  const int m0 = ((lq + T::BM - 1) / T::BM - 1 - (int)(local / (uint32_t)n_heads)) * T::BM;
+  it.q_start = sq.q_start + m0;
+  it.q_rows = lq - m0 < T::BM ? lq - m0 : T::BM;
+  it.kv_start = sq.kv_start;
+
+  // Keys under lim are all that any row sees; a row sees keys under its klim.
+  const int pos0 = m0 + lk - lq;
+  int lim = lk;
+  if (p.causal) {
+    const int last = pos0 + it.q_rows > sq.prefix ? pos0 + it.q_rows : sq.prefix;
+    lim = last < lk ? last : lk;
+  }
+  auto row_limit = [&](int row) {
+    if (!p.causal) return lim;
+    const int k = pos0 + row + 1 > sq.prefix ? pos0 + row + 1 : sq.prefix;
+    return k < lim ? k : lim;
+  };
+  int qrow = L.wave * 32 + L.l32;
+  const bool row_valid = qrow < it.q_rows;
+  if (!row_valid) qrow = it.q_rows - 1;
+  int klim = row_limit(qrow);
+  const int klim_first = row_limit(0);
+  const int wave_last = L.wave * 32 + 31 < it.q_rows ? L.wave * 32 + 31 : it.q_rows - 1;
+  const int klim_wave = __builtin_amdgcn_readfirstlane(row_limit(wave_last));
+
+  LiveTiles tiles;
+  tiles.ranges = nullptr;
+  tiles.base = -64;
+  tiles.live = tiles.pure = 0;
+  const int nt = lim > 0 ? (lim + T::BN - 1) / T::BN : 0;
+  const int64_t part_end = ((int64_t)it.part + 1) * p.part_tiles;
+  int t = nt;
+  if ((int64_t)it.part * p.part_tiles < nt) t = it.part * p.part_tiles;
+  tiles.end = part_end < nt ? (int)part_end : nt;
+  const bool have_docs = p.q_doc != nullptr;
+  int doc = 0;
+  const int32_t* kdoc = nullptr;
+  if (have_docs) {
+    kdoc = p.k_doc + sq.kv_start;
+    doc = p.q_doc[it.q_start + qrow];
+    if (doc < 0) klim = 0;  // sees nothing
+    const DocTile a = doc_range(p.q_doc + it.q_start, it.q_rows < 64 ? it.q_rows : 64);
+    const DocTile b = it.q_rows > 64 ? doc_range(p.q_doc + it.q_start + 64, it.q_rows - 64) : a;
+    tiles.mine.lo = a.lo < b.lo ? a.lo : b.lo;
+    tiles.mine.hi = a.hi > b.hi ? a.hi : b.hi;
+    tiles.mine.any_lo = a.any_lo < b.any_lo ? a.any_lo : b.any_lo;
+    tiles.ranges = p.doc_tiles + sq.tile0;
+  }
+  t = tiles.next(t);
+
+  f32x16 o[T::NDB];
+#pragma unroll
+  for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  RowState r = {kNoReference, 0.f, 0.f};
+  bool poison = false;
+
+  if (t < tiles.end) {
+    const int kv_head = it.head / p.group;
+    const char* kbase = static_cast<const char*>(p.k) + (int64_t)it.kv_start * p.k_stride_b + (int64_t)kv_head * T::ROW_B;
+    const char* vbase = static_cast<const char*>(p.v) + (int64_t)it.kv_start * p.v_stride_b + (int64_t)kv_head * T::ROW_B;
+    const float c = CAP || BIAS ? 1.f : p.c_log2;
+    const float slope = BIAS ? p.slopes[it.head] * 1.44269504088896340736f : 0.f;
+
+    auto load = [&](int ti, int slot) {
+      const int key0 = tile_first_key<T>(ti, lim);
+      tile_load_one<T>(kbase, p.k_stride_b, key0, lim, L.lrow, L.kcol, L.kvoff, smem, T::K_OFF + slot * T::TILE_B, L.wave);
+      tile_load_one<T>(vbase, p.v_stride_b, key0, lim, L.lrow, L.vcol, vvoff, smem, T::V_OFF + slot * T::TILE_B, L.wave);
+      if (have_docs && L.wave == 0) {
+        const int last = lim - 1 - key0;
+        lds_dma_4(kdoc + key0, (uint32_t)(L.lane < last ? L.lane : last) * 4u, lds + kDocsOff<T> + slot * (T::BN * 4));
+      }
+    };
+    const uint32_t spare = lds + (L.wave < 2 ? T::K_OFF : T::V_OFF) + T::TILE_B + (uint32_t)(L.wave % 2) * (32 * T::ROW_B);
+    static_assert(T::TILE_B == 2 * 32 * T::ROW_B, "two wavefronts' rows in a tile");
+    q_rows_load<T>(p, L, it, p.q_stride_b, (int64_t)it.head * T::ROW_B, spare);
+    load(t, 0);
+    if (tid < 6) *(lds_u32*)(uintptr_t)(lds + kBadOff<T> + tid * 4) = 0;
+    wait_loads();
+    bf16x8 qf[T::NKS];
+    q_rows_read<T>(p, L, spare, qf);
+    wg_barrier();
+    int ka[T::NKS], va[T::NDB];
+    L.operand_addrs(lds, lds, ka, va);
+    int slot = 0, turn = 0;  // of the K / V buffers and of the bad-key masks
+    const TailRows tail = tail_rows<T>(lim);
+
+    while (t < tiles.end) {
+      const int key0 = tile_first_key<T>(t, lim);
+      const bool last = t == nt - 1;
+      const int lo = last ? tail.lo : 0;
+      // Some pair of a row of the item and a key of the tile is dead.
+      const bool masked = (last && tail.hi - tail.lo != T::BN) || klim_first < key0 + T::BN || !tiles.is_pure(t);
+      const int tn = tiles.next(t + 1);
+      wait_loads();
+      const uint32_t bad_at = lds + kBadOff<T> + (uint32_t)turn * 8u;
+      if (masked) {
+        const uint32_t found = make_finite<T::LPT>(lds + T::V_OFF + slot * T::TILE_B + L.wave * 1024 + L.lane * 16, T::NWAVES * 1024);
+        if (found != 0) {
+#pragma unroll
+          for (int i = 0; i < T::LPT; ++i) {
+            const int row = i * T::GROUP + L.lrow;
+            if (found >> i & 1) __hip_atomic_fetch_or((lds_u32*)(uintptr_t)(bad_at + (uint32_t)(row >> 5) * 4u), 1u << (row & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          }
+        }
+      }
+      wg_barrier();
+      if (tn < tiles.end) load(tn, slot ^ 1);
+      if (tid < 2) *(lds_u32*)(uintptr_t)(lds + kBadOff<T> + (uint32_t)(turn == 0 ? 2 : turn - 1) * 8u + tid * 4) = 0;
+      if (key0 + lo < klim_wave) {  // a wavefront none of whose rows sees the tile skips it
+        f32x16 s[T::NKB];
+        uint32_t pb[T::NKB][8];
+        mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, s);
+        if constexpr (CAP || BIAS) shape_scores<T::NKB, CAP, BIAS>(s, p, slope, pos0 + qrow - key0 - 4 * L.hh);
+        if (masked) {
+          const int n = klim - key0 - lo;
+          const LaneMask m = {lo - 4 * L.hh, n > 0 ? (unsigned)n : 0u};
+          const uint64_t bad = (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)bad_at) |
+                               (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)(bad_at + 4)) << 32;
+          poison |= mask_scores<T::NKB>(s, m, have_docs, lds + kDocsOff<T> + slot * (T::BN * 4), doc, L.hh, bad);
+        }
+        scores_ready<T>(s);
+        const float mx = tile_max<T>(s);
+        masked_softmax<T::NKB, T::NDB, LSE>(s, mx, c, pb, o, r);
+        mfma_stream<T, true, 0, 0, kPrefetch>(smem, va, ka, pb, qf, o, s);
+        r.l += row_sum<T>(pb);
+      }
+#pragma unroll
+      for (int ks = 0; ks < T::NKS; ++ks) ka[ks] ^= T::TILE_B;
+#pragma unroll
+      for (int db = 0; db < T::NDB; ++db) va[db] ^= T::TILE_B;
+      slot ^= 1;
+      turn = turn == 2 ? 0 : turn + 1;
+      t = tn;
+    }
+    if (__builtin_amdgcn_ballot_w64(poison) != 0) {
+      const int k0 = it.part * p.part_tiles * T::BN;
+      add_not_finite<T>(p, vbase, kdoc, k0, tiles.end * T::BN < lim ? tiles.end * T::BN : lim, T::BN, T::BN, klim, doc, L.hh, o);
+    }
+    wg_barrier();  // the rows are staged in the K buffers
+  }
+
+  const float l = r.l + __shfl_xor(r.l, 32), lx = r.lx + __shfl_xor(r.lx, 32);
+  const bool any = l > 0.f || l != l;
+  store_rows<T>(p, L, it, o, any ? 1.f / l : 0.f, lds + T::K_OFF + (uint32_t)L.wave * (32 * T::ROW_B));
+  if constexpr (LSE) {
+    if (row_valid && L.hh == 0) {
+      const float c = CAP || BIAS ? 1.f : p.c_log2;
+      float* dst = p.part_out != nullptr ? p.part_lse + (int64_t)it.part * p.part_rows * n_heads : p.lse;
+      dst[(int64_t)(it.q_start + qrow) * n_heads + it.head] = any ? kLn2 * (r.m_ref * c + __builtin_amdgcn_logf(lx)) : -__builtin_inff();
+    }
+  }
+#endif
+}
+
+// ---------------------------------------------------------------------------------------------
+// Few query rows (one new token, say): every (row, query head of a key head's group) is a column, at most 32 of them, so that
+// K and V are read once for the whole group.  Bound by reading them.  The four wavefronts take 32-key blocks in turn, each
+// with loads, LDS and softmax state of its own and no barrier until the end, when their four results are joined.
+// ---------------------------------------------------------------------------------------------
+template <int D>
+struct FewRows {
+  using T = Tile<D, 4, 32>;
+  static constexpr int STAGES = D == 128 ? 2 : 4;
+  static constexpr int BLOCK_B = 32 * T::ROW_B;          // 32 keys of K or V
+  static constexpr int WAVE_B = STAGES * 2 * BLOCK_B;    // [stage][K, V]
+  static constexpr int DOCS_OFF = 4 * WAVE_B;            // [wave][stage][32] ids
+  static constexpr int STATE_OFF = DOCS_OFF + 4 * STAGES * 128;  // [m, l, lx][wave][column]
+  static constexpr int LDS_BYTES = STATE_OFF + 3 * 4 * 32 * 4;
+  static constexpr int N = 32 / T::RPI;                  // load instructions of a block of K or V
+  static_assert(32 * D * 4 <= WAVE_B, "a wavefront's result fits its stages");
+};
+
+template <int D, bool CAP, bool BIAS>
+__global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(1, 1))) masked_few_rows_kernel(MaskedParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  using F = FewRows<D>;
+  using T = typename F::T;
+  extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+  lds_char* smem = (lds_char*)smem_generic;
+  const uint32_t lds = (uint32_t)(uintptr_t)smem;
+  const int tid = threadIdx.x;
+  Lane<T> L;
+  L.init(tid, p.k_stride_b);
+  const int wave = L.wave, hh = L.hh;
+
+  const MaskedSeq& sq = find_seq(p, blockIdx.x, false);
+  const int lq = sq.q_len, lk = sq.kv_len, group = p.group, n_heads = p.n_heads;
+  uint32_t local = blockIdx.x - sq.first;
+  const int part = (int)(local % (uint32_t)p.n_parts), kv_head = (int)(local / (uint32_t)p.n_parts);
+  const int n_cols = lq * group;
+  const int col = L.l32 < n_cols ? L.l32 : n_cols - 1, row = col / group, head = kv_head * group + (col - row * group);
+
+  const int pos0 = lk - lq;
+  auto row_limit = [&](int i) {
+    if (!p.causal) return lk;
+    const int k = pos0 + i + 1 > sq.prefix ? pos0 + i + 1 : sq.prefix;
+    return k < lk ? k : lk;
+  };
+  const int lim = row_limit(lq - 1), klim_first = row_limit(0);
+  int klim = row_limit(row);
+
+  LiveTiles tiles;
+  tiles.ranges = nullptr;
+  tiles.base = -64;
+  tiles.live = tiles.pure = 0;
+  const int nt = lim > 0 ? (lim + 63) / 64 : 0;
+  const int64_t part_end = ((int64_t)part + 1) * p.part_tiles;
+  int t0 = nt;
+  if ((int64_t)part * p.part_tiles < nt) t0 = part * p.part_tiles;
+  tiles.end = part_end < nt ? (int)part_end : nt;
+  const bool have_docs = p.q_doc != nullptr;
+  int doc = 0;
+  const int32_t* kdoc = nullptr;
+  if (have_docs) {
+    kdoc = p.k_doc + sq.kv_start;
+    doc = p.q_doc[sq.q_start + row];
+    if (doc < 0) klim = 0;  // sees nothing
+    tiles.mine = doc_range(p.q_doc + sq.q_start, lq);
+    tiles.ranges = p.doc_tiles + sq.tile0;
+  }
+  // Blocks of 32 keys; this wavefront's are wave, wave + 4, ... of those in live tiles.
+  const int n_blocks = tiles.end * 2 < (lim + 31) / 32 ? tiles.end * 2 : (lim + 31) / 32;
+  auto next_block = [&](int b) {
+    while (b < n_blocks) {
+      const int t = tiles.next(b >> 1);
+      if (t == b >> 1) return b;
+      b += (2 * t - b + 3) & ~3;
+    }
+    return n_blocks;
+  };
+  const int first_block = t0 * 2 + ((wave - t0 * 2) & 3);
+
+  f32x16 o[T::NDB];
+#pragma unroll
+  for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  RowState r = {kNoReference, 0.f, 0.f};
+  const float c = CAP || BIAS ? 1.f : p.c_log2;
+  const uint32_t ring = lds + (uint32_t)wave * F::WAVE_B, docs = lds + F::DOCS_OFF + (uint32_t)wave * (F::STAGES * 128);
+
+  int block = t0 < tiles.end ? next_block(first_block) : n_blocks;
+  if (block < n_blocks) {
+    const char* kbase = static_cast<const char*>(p.k) + (int64_t)sq.kv_start * p.k_stride_b + (int64_t)kv_head * T::ROW_B;
+    const char* vbase = static_cast<const char*>(p.v) + (int64_t)sq.kv_start * p.v_stride_b + (int64_t)kv_head * T::ROW_B;
+    const float slope = BIAS ? p.slopes[head] * 1.44269504088896340736f : 0.f;
+    const int at = L.lane % T::CPR, q = L.lane / T::CPR;  // chunk and row of this lane in one load instruction
+    const uint32_t vcol = (uint32_t)((at ^ T::swz_v(q)) * 16);
+
+    auto load = [&](int b, int stage) {
+      const int key0 = b * 32, last = lim - 1 - key0;
+      const uint32_t dst = ring + (uint32_t)stage * (2 * F::BLOCK_B);
+      const char* kb = kbase + (int64_t)key0 * p.k_stride_b;
+      const char* vb = vbase + (int64_t)key0 * p.v_stride_b;
+#pragma unroll
+      for (int i = 0; i < F::N; ++i) {
+        int rr = i * T::RPI + q;
+        const uint32_t kcol = (uint32_t)((at ^ T::swz_k(rr)) * 16);
+        rr = rr < last ? rr : last;
+        lds_dma_16(kb, (uint32_t)rr * (uint32_t)p.k_stride_b + kcol, dst + i * 1024);
+        lds_dma_16(vb, (uint32_t)rr * (uint32_t)p.v_stride_b + vcol, dst + F::BLOCK_B + i * 1024);
+      }
+      if (have_docs) {
+        const int k = L.l32 < last ? L.l32 : last;
+        if (L.hh == 0) lds_dma_4(kdoc + key0, (uint32_t)k * 4u, docs + (uint32_t)stage * 128u);
+      }
+    };
+
+    bf16x8 qf[T::NKS];
+    {
+      const char* qp = static_cast<const char*>(p.q) + (int64_t)(sq.q_start + row) * p.q_stride_b + (int64_t)head * T::ROW_B + hh * 16;
+#pragma unroll
+      for (int ks = 0; ks < T::NKS; ++ks) {
+        u32x4 w = *reinterpret_cast<const u32x4*>(qp + ks * 32);
+        if (p.negate) w ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        qf[ks] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    int ka[T::NKS], va[T::NDB];
+    bool poison = false;
+    // The blocks in flight, oldest first, and whether every row sees all of their keys' documents; n_blocks stands for none.
+    int queue[F::STAGES];
+    bool pure[F::STAGES];
+    auto take = [&](int i, int b, int to_stage) {
+      queue[i] = b;
+      pure[i] = b < n_blocks && tiles.is_pure(b >> 1);
+      if (b < n_blocks) load(b, to_stage);
+    };
+    take(0, block, 0);
+#pragma unroll
+    for (int i = 1; i < F::STAGES; ++i) take(i, queue[i - 1] < n_blocks ? next_block(queue[i - 1] + 4) : n_blocks, i);
+    int stage = 0;
+    while (queue[0] < n_blocks) {
+      // The oldest block has landed when at most the later ones' loads are outstanding.
+      if (queue[F::STAGES - 1] < n_blocks) {
+        if (have_docs) wait_loads_but<(F::STAGES - 1) * (2 * F::N + 1)>();
+        else wait_loads_but<(F::STAGES - 1) * 2 * F::N>();
+      } else {
+        wait_loads();
+      }
+      const int key0 = queue[0] * 32;
+      const uint32_t kbuf = ring + (uint32_t)stage * (2 * F::BLOCK_B), vbuf = kbuf + F::BLOCK_B;
+      const bool masked = klim_first < key0 + 32 || !pure[0];
+      uint32_t bad = 0;
+      if (masked) {
+        const uint32_t found = make_finite<F::N>(vbuf + (uint32_t)L.lane * 16u, 1024);
+        if (__builtin_amdgcn_ballot_w64(found != 0) != 0) {
+#pragma unroll
+          for (int i = 0; i < F::N; ++i) {
+            const uint64_t rows = __builtin_amdgcn_ballot_w64((found >> i & 1) != 0);
+#pragma unroll
+            for (int k = 0; k < T::RPI; ++k)
+              if ((rows >> (k * T::CPR)) & ((1ull << T::CPR) - 1)) bad |= 1u << (i * T::RPI + k);
+          }
+        }
+        asm volatile("" ::: "memory");
+      }
+      L.operand_addrs(kbuf - T::K_OFF, vbuf - T::V_OFF, ka, va);
+      f32x16 s[1];
+      uint32_t pb[1][8];
+      mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, s);
+      if constexpr (CAP || BIAS) shape_scores<1, CAP, BIAS>(s, p, slope, pos0 + row - key0 - 4 * hh);
+      if (masked) {
+        const int n = klim - key0;
+        const LaneMask m = {-4 * hh, n > 0 ? (unsigned)n : 0u};
+        poison |= mask_scores<1>(s, m, have_docs, docs + (uint32_t)stage * 128u, doc, hh, bad);
+      }
+      asm volatile("s_nop 11" : "+v"(s[0]));  // as scores_ready
+      const float mx = tile_max<T>(s);
+      masked_softmax<1, T::NDB, true>(s, mx, c, pb, o, r);
+      mfma_stream<T, true, 0, 0, kPrefetch>(smem, va, ka, pb, qf, o, s);
+      r.l += row_sum<T>(pb);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this stage has been read
+      const int youngest = queue[F::STAGES - 1];
+#pragma unroll
+      for (int i = 0; i + 1 < F::STAGES; ++i) {
+        queue[i] = queue[i + 1];
+        pure[i] = pure[i + 1];
+      }
+      take(F::STAGES - 1, youngest < n_blocks ? next_block(youngest + 4) : n_blocks, stage);
+      stage = stage == F::STAGES - 1 ? 0 : stage + 1;
+    }
+    if (__builtin_amdgcn_ballot_w64(poison) != 0)
+      add_not_finite<T>(p, vbase, kdoc, first_block * 32, n_blocks * 32 < lim ? n_blocks * 32 : lim, 32, 128, klim, doc, hh, o);
+  }
+
+  // The four results, unnormalised, through the wavefronts' own stages: 16-byte chunk j of column i at j ^ i.
+  constexpr int CH = D / 4;
+#pragma unroll
+  for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int ch = 8 * db + 2 * g + hh;
+      const f32x4 f = {o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
+      *(lds_u32x4*)(uintptr_t)(ring + (uint32_t)(L.l32 * (D * 4) + ((ch ^ (L.l32 & (CH - 1))) * 16))) = __builtin_bit_cast(u32x4, f);
+    }
+  typedef __attribute__((address_space(3))) float lds_f32;
+  const uint32_t state = lds + F::STATE_OFF;
+  const float l = r.l + __shfl_xor(r.l, 32), lx = r.lx + __shfl_xor(r.lx, 32);
+  if (hh == 0) {
+    *(lds_f32*)(uintptr_t)(state + (uint32_t)(wave * 32 + L.l32) * 4u) = l > 0.f || l != l ? r.m_ref * c : -__builtin_inff();
+    *(lds_f32*)(uintptr_t)(state + (uint32_t)(128 + wave * 32 + L.l32) * 4u) = l;
+    *(lds_f32*)(uintptr_t)(state + (uint32_t)(256 + wave * 32 + L.l32) * 4u) = lx;
+  }
+  wg_barrier();
+  for (int e = tid; e < n_cols * CH; e += 256) {
+    const int cc = e / CH, ch = e % CH;
+    float m[4], w[4], top = -__builtin_inff(), sum = 0.f, sumx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = *(lds_f32*)(uintptr_t)(state + (uint32_t)(i * 32 + cc) * 4u);
+      top = __builtin_fmaxf(top, m[i]);
+    }
+    if (top == -__builtin_inff()) top = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = __builtin_amdgcn_exp2f(m[i] - top);
+      sum = __builtin_fmaf(w[i], *(lds_f32*)(uintptr_t)(state + (uint32_t)(128 + i * 32 + cc) * 4u), sum);
+      sumx = __builtin_fmaf(w[i], *(lds_f32*)(uintptr_t)(state + (uint32_t)(256 + i * 32 + cc) * 4u), sumx);
+      const f32x4 f = __builtin_bit_cast(f32x4, *(lds_u32x4*)(uintptr_t)(lds + (uint32_t)(i * F::WAVE_B + cc * (D * 4) + ((ch ^ (cc & (CH - 1))) * 16))));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[k] = __builtin_fmaf(w[i], f[k], acc[k]);
+    }
+    const bool any = sum > 0.f || sum != sum;
+    const float inv = any ? 1.f / sum : 0.f;
+    const int rr = cc / group, hd = kv_head * group + (cc - rr * group);
+    const int64_t rh = (int64_t)(sq.q_start + rr) * n_heads + hd;
+    const float row_lse = any ? kLn2 * (top + __builtin_amdgcn_logf(sumx)) : -__builtin_inff();
+    if (p.part_out != nullptr) {
+      const int64_t prh = (int64_t)part * p.part_rows * n_heads + rh;
+      const f32x4 y = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+      store_through(reinterpret_cast<u32x4*>(p.part_out + prh * D + ch * 4), __builtin_bit_cast(u32x4, y));
+      if (ch == 0) p.part_lse[prh] = row_lse;
+    } else {
+      const u32x2 y = {pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+      *reinterpret_cast<u32x2*>(static_cast<char*>(p.out) + rh * (2 * D) + ch * 8) = y;
+      if (ch == 0 && p.lse != nullptr) p.lse[rh] = row_lse;
+    }
+  }
+#endif
+}
+
+// ---------------------------------------------------------------------------------------------
+// out = sum over parts exp(lse_part - lse) O_part,  eight elements a thread.  Bound by the parts, which lie in the memory-side cache.
+// ---------------------------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256) masked_join_kernel(const float* part_out, const float* part_lse, void* out, float* lse, int64_t n_rh,
+                                                          int n_parts) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, rh = e / (D / 8);
+  if (rh >= n_rh) return;
+  float top = -__builtin_inff();
+  for (int i = 0; i < n_parts; ++i) top = __builtin_fmaxf(top, part_lse[i * n_rh + rh]);
+  if (top == -__builtin_inff()) top = 0.f;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+  for (int i = 0; i < n_parts; ++i) {
+    const float w = __builtin_amdgcn_exp2f((part_lse[i * n_rh + rh] - top) * 1.44269504088896340736f);
+    const f32x4* src = reinterpret_cast<const f32x4*>(part_out + (i * n_rh * D + e * 8));
+    const f32x4 a = src[0], b = src[1];
+    sum += w;
+    if (w != 0.f)  // a part without keys has left its values unwritten or zero
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        acc[k] = __builtin_fmaf(w, a[k], acc[k]);
+        acc[4 + k] = __builtin_fmaf(w, b[k], acc[4 + k]);
+      }
+  }
+  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+  u32x4 y;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) y[k] = pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
+  store_through(reinterpret_cast<u32x4*>(out) + e, y);
+  if (lse != nullptr && (e & (D / 8 - 1)) == 0)
+    lse[rh] = sum > 0.f || sum != sum ? top + kLn2 * __builtin_amdgcn_logf(sum) : -__builtin_inff();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Launch
+// ---------------------------------------------------------------------------------------------
+using MaskedKernel = void (*)(MaskedParams);
+struct MaskedEntry {
+  MaskedKernel fn;
+  int lds;
+};
+
+template <int D, bool CAP, bool BIAS>
+static MaskedEntry entry_of(bool few_rows, bool lse) {
+  using T = Tile<D, 4, 64>;
+  if (few_rows) return {masked_few_rows_kernel<D, CAP, BIAS>, FewRows<D>::LDS_BYTES};
+  if (lse) return {masked_attn_kernel<T, CAP, BIAS, true>, kMaskedLds<T>};
+  return {masked_attn_kernel<T, CAP, BIAS, false>, kMaskedLds<T>};
+}
+template <int D>
+static MaskedEntry entry_of(const MaskedKind& k) {
+  if (k.cap) return k.bias ? entry_of<D, true, true>(k.few_rows, k.lse) : entry_of<D, true, false>(k.few_rows, k.lse);
+  return k.bias ? entry_of<D, false, true>(k.few_rows, k.lse) : entry_of<D, false, false>(k.few_rows, k.lse);
+}
+static MaskedEntry entry_of(const MaskedKind& k) { return k.head_dim == 64 ? entry_of<64>(k) : entry_of<128>(k); }
+
+hipError_t masked_attn_prepare() {
+  for (int i = 0; i < 32; ++i) {
+    const MaskedKind k = {i & 1 ? 128 : 64, (i & 2) != 0, (i & 4) != 0, (i & 8) != 0, (i & 16) != 0};
+    const MaskedEntry m = entry_of(k);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(m.fn), hipFuncAttributeMaxDynamicSharedMemorySize, m.lds);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t masked_attn_launch(const MaskedParams& p, const MaskedKind& kind, uint32_t n_doc_tiles, hipStream_t stream) {
+  if (p.n_items == 0) return hipSuccess;
+  if (n_doc_tiles > 0) {
+    hipLaunchKernelGGL(masked_doc_tiles_kernel, dim3((n_doc_tiles + 3) / 4), dim3(256), 0, stream, p, n_doc_tiles);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const MaskedEntry m = entry_of(kind);
+  hipLaunchKernelGGL(m.fn, dim3(p.n_items), dim3(256), m.lds, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t masked_join_launch(const MaskedParams& p, int head_dim, hipStream_t stream) {
+  const int64_t n_rh = p.part_rows * p.n_heads, blocks = (n_rh * (head_dim / 8) + 255) / 256;
+  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const auto fn = head_dim == 64 ? masked_join_kernel<64> : masked_join_kernel<128>;
+  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(256), 0, stream, p.part_out, p.part_lse, p.out, p.lse, n_rh, p.n_parts);
+  return hipGetLastError();
+}
+
+}  // namespace dit

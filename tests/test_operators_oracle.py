@@ -1,0 +1,121 @@
+"""Pins of the oracle of the rotation table, the norm and rotation, and masked attention; the binding's own checks (no GPU)."""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2604_04335_amd as da
+from oracle import operators_oracle as orc
+
+
+def _rng(seed):
+    return np.random.Generator(np.random.PCG64(seed))
+
+
+def test_frequencies_by_hand():
+    f, axis = orc.frequencies([4, 2], [100.0, 7.0], "plain", [1.0, 1.0])
+    assert np.allclose(f, [1.0, 0.1, 1.0]) and axis.tolist() == [0, 0, 1]
+    assert np.allclose(orc.frequencies([4], [100.0], "linear", [4.0])[0], [0.25, 0.025])
+    # base: (100 * 4^2)^(-1/2) = 1/40: the last pair is squeezed by exactly the factor, the first not at all
+    assert np.allclose(orc.frequencies([4], [100.0], "base", [4.0])[0], [1.0, 0.1 / 4.0])
+    assert np.allclose(orc.frequencies([2], [100.0], "base", [4.0])[0], [1.0])
+    # bands: turns over 2 pi * 100 positions are 100 and 10; between 5 and 15 the blend of 10 is a half
+    f = orc.frequencies([4], [100.0], "bands", [4.0], [2.0 * math.pi * 100.0], low=5.0, high=15.0)[0]
+    assert np.allclose(f, [1.0, 0.1 * (0.5 + 0.5 / 4.0)])
+
+
+def test_rotation_keeps_relative_positions():
+    """<R(p) x, R(q) y> depends on p - q only, in both layouts, and norms are kept."""
+    rng = _rng(3)
+    f, axis = orc.frequencies([16], [10000.0], "plain", [1.0])
+    x, y = rng.standard_normal((2, 1, 1, 24))
+    for half in (False, True):
+        def turned(z, p):
+            return orc.norm_rope(z, "none", 0.0, None, None, orc.rope_table(np.array([[p]]), f, axis), 16, half)[0][0, 0]
+        assert np.allclose(turned(x, 7) @ turned(y, 3), turned(x, 1007) @ turned(y, 1003))
+        assert np.allclose(np.linalg.norm(turned(x, 123)), np.linalg.norm(x))
+        assert np.array_equal(turned(x, 9)[16:], x[0, 0, 16:])
+        assert np.allclose(turned(x, 0), x[0, 0])
+
+
+def test_rotation_by_hand():
+    x = np.arange(1.0, 9.0).reshape(1, 1, 8)
+    table = np.array([[[0.0, 1.0], [0.0, -1.0]]])  # a quarter turn, and one back
+    assert orc.norm_rope(x, "none", 0, None, None, table, 4, False)[0][0, 0].tolist() == [-2, 1, 4, -3, 5, 6, 7, 8]
+    assert orc.norm_rope(x, "none", 0, None, None, table, 4, True)[0][0, 0].tolist() == [-3, 4, 1, -2, 5, 6, 7, 8]
+
+
+def test_norms_by_hand():
+    x = np.array([[[3.0, 4.0, 0.0, 0.0]]])
+    assert np.allclose(orc.norm_rope(x, "rms", 0.0, None, None, None, 0, False)[0][0, 0], np.array([3, 4, 0, 0]) / 2.5)
+    y = orc.norm_rope(x, "layer", 0.0, np.array([1, 1, 2, 2.0]), np.array([0, 0, 0, 1.0]), None, 0, False)[0][0, 0]
+    d = np.array([1.25, 2.25, -1.75, -1.75])
+    d = d / np.sqrt((d * d).mean())
+    assert np.allclose(y, [d[0], d[1], 2 * d[2], 2 * d[3] + 1])
+
+
+def test_masked_attention_against_a_sum_over_pairs():
+    rng = _rng(11)
+    cu_q, cu_k, H, G, D = [0, 3, 3, 5], [0, 4, 6, 7], 4, 2, 6
+    q, k, v = rng.standard_normal((5, H, D)), rng.standard_normal((7, G, D)), rng.standard_normal((7, G, D))
+    slopes, prefix = rng.random(H), [2, 0, 0]
+    q_doc, k_doc = np.array([0, 1, -1, 5, 5]), np.array([0, 1, 0, 1, 9, 9, 5])
+    out, lse, spread, top = orc.masked_attention(q, k, v, cu_q, cu_k, 0.7, causal=True, prefix=prefix, cap=2.0, slopes=slopes, q_doc=q_doc,
+                                                 k_doc=k_doc)
+    for i in range(3):
+        lq, lk = cu_q[i + 1] - cu_q[i], cu_k[i + 1] - cu_k[i]
+        for r in range(lq):
+            for h in range(H):
+                num, den, ab = np.zeros(D), 0.0, np.zeros(D)
+                for j in range(lk):
+                    pos = r + lk - lq
+                    a, b = q_doc[cu_q[i] + r], k_doc[cu_k[i] + j]
+                    if a != b or a < 0 or not (j <= pos or j < prefix[i]):
+                        continue
+                    s = 2.0 * math.tanh(0.7 * float(q[cu_q[i] + r, h] @ k[cu_k[i] + j, h // 2]) / 2.0) - slopes[h] * abs(pos - j)
+                    num += math.exp(s) * v[cu_k[i] + j, h // 2]
+                    ab += math.exp(s) * abs(v[cu_k[i] + j, h // 2])
+                    den += math.exp(s)
+                row = cu_q[i] + r
+                if den:
+                    assert np.allclose(out[row, h], num / den) and np.isclose(lse[row, h], math.log(den))
+                    assert np.allclose(spread[row, h], ab / den)
+                else:
+                    assert not out[row, h].any() and lse[row, h] == -np.inf
+    assert lse[2].max() == -np.inf  # the row without a document
+
+
+def test_visible_by_hand():
+    assert orc.visible(2, 4, True, 0, None, None).astype(int).tolist() == [[1, 1, 1, 0], [1, 1, 1, 1]]
+    assert orc.visible(3, 2, True, 0, None, None).astype(int).tolist() == [[0, 0], [1, 0], [1, 1]]
+    assert orc.visible(3, 2, True, 1, None, None).astype(int).tolist() == [[1, 0], [1, 0], [1, 1]]
+    ids = np.array([4, -1, 4, 7])
+    assert orc.visible(4, 4, False, 0, ids, ids).astype(int).tolist() == [[1, 0, 1, 0], [0, 0, 0, 0], [1, 0, 1, 0], [0, 0, 0, 1]]
+
+
+def test_binding_structures():
+    spec = da.RopeSpec([16, 56, 56], theta=[256.0, 1e4, 1e4], scaling=da.ROPE_LINEAR, factor=2.0)
+    assert spec.rot_dim == 128 and list(spec.theta[:3]) == [256.0, 1e4, 1e4] and list(spec.factor[:3]) == [2.0] * 3
+    with pytest.raises(ValueError):
+        da.RopeSpec([16, 16], theta=[1.0, 2.0, 3.0])
+    with pytest.raises(ValueError):
+        da.RopeSpec([])
+    import torch
+    t = torch.zeros((5, 12 * 64), dtype=torch.bfloat16)
+    side = da.NormHeads(t[:, :256].unflatten(1, (4, 64)), torch.zeros((5, 4, 64), dtype=torch.bfloat16))
+    assert side.row_stride == 768 and side.out_row_stride == 256 and side.n_heads == 4
+    one = torch.zeros((1, 4, 64), dtype=torch.bfloat16)
+    assert da.NormHeads(one, one).row_stride == 256
+    for bad in (torch.zeros((5, 4, 64)), torch.zeros((5, 64, 4), dtype=torch.bfloat16).transpose(1, 2),
+                torch.zeros((4, 5, 64), dtype=torch.bfloat16).transpose(0, 1)):
+        with pytest.raises(ValueError):
+            da.NormHeads(bad, one)
+    mask = da.AttnMask(causal=True, prefix=[3, 4])
+    assert mask.causal == 1 and mask.prefix[1] == 4
+    x = torch.zeros((8, 1, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):  # a prefix for two of three sequences
+        da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 2, 4, 8], None, 1, 1, 64, 1.0, mask, x)
+    with pytest.raises(ValueError):  # key boundaries of fewer sequences
+        da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 2, 8], [0, 8], 1, 1, 64, 1.0, None, x)
+    with pytest.raises(da.DitAttnError):
+        da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 8], None, 1, 1, 64, 1.0, None, x)
