@@ -34,6 +34,7 @@ struct MaskedParams : AttnParams {
   float c_true;            // |scale| * log2(e)
   float tanh_in;           // 2 * log2(e) * |scale| / cap
   float cap_log2;          // cap * log2(e)
+  float small, poly[4];    // cap: raw scores up to `small` take s (poly[0] + poly[1] s^2 + poly[2] s^4 + poly[3] s^6)
   int32_t causal;
   int32_t group;           // query heads per key head
   int32_t n_parts;         // parts per sequence

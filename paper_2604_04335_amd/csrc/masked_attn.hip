@@ -95,25 +95,43 @@ struct LiveTiles {
 // Scores of a lane: element i of block kb is key 32 kb + 8 (i / 4) + (i % 4) + 4 hh of the tile.
 __device__ __forceinline__ constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i >> 2) + (i & 3); }
 
+// C tanh(s / C) log2(e) of a raw score: tanh y = 1 - 2 / (exp(2 y) + 1), whose limits need no clamp.
+__device__ __forceinline__ float capped(const MaskedParams& p, float x) {
+  const float e = __builtin_amdgcn_exp2f(x * p.tanh_in);
+  return __builtin_fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
+}
+
 // Raw scores -> base-2 exponents, with the cap and the bias.  at: pos - first key of the tile - 4 hh of this lane.
+// small (the same in the whole wavefront): no raw score exceeds p.small, and the cap is a polynomial: five instructions a score
+// instead of three and an exponential and a reciprocal, which take four times as long each.
 template <int NKB, bool CAP, bool BIAS>
-__device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParams& p, float slope_log2, int at) {
-  const float base = (float)at;
+__device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParams& p, bool small, float slope_log2, int at) {
+  if constexpr (CAP) {
+    if (small) {
 #pragma unroll
-  for (int kb = 0; kb < NKB; ++kb)
+      for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x = s[kb][i];
-      if constexpr (CAP) {
-        // tanh y = 1 - 2 / (exp(2 y) + 1), whose limits need no clamp
-        const float e = __builtin_amdgcn_exp2f(x * p.tanh_in);
-        x = __builtin_fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
-      } else {
-        x *= p.c_true;
-      }
-      if constexpr (BIAS) x = __builtin_fmaf(-slope_log2, __builtin_fabsf(base - (float)key_of(kb, i)), x);
-      s[kb][i] = x;
+        for (int i = 0; i < 16; ++i) {
+          const float x = s[kb][i], z = x * x;
+          s[kb][i] = x * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, p.poly[3], p.poly[2]), p.poly[1]), p.poly[0]);
+        }
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = capped(p, s[kb][i]);
     }
+  }
+  if constexpr (BIAS) {
+    const float base = (float)at;
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = CAP ? s[kb][i] : s[kb][i] * p.c_true;
+        s[kb][i] = __builtin_fmaf(-slope_log2, __builtin_fabsf(base - (float)key_of(kb, i)), x);
+      }
+  }
 }
 
 // What a lane's row sees of a tile: keys lo <= key < hi of it, less 4 hh, whose ids are `doc` if there are ids.
@@ -128,26 +146,39 @@ typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
 
-// Dead scores := -inf.  docs: LDS byte of the tile's ids (0 with no ids), hh as everywhere.  With bad != 0 (bits: keys with a
-// value that is not finite) returns whether this lane's row sees one of them.
+// Dead scores := -inf.  docs: LDS byte of the tile's ids, hh as everywhere.
 template <int NKB>
-__device__ __forceinline__ bool mask_scores(f32x16 (&s)[NKB], LaneMask m, bool have_docs, uint32_t docs, int doc, int hh, uint64_t bad) {
-  bool sees_bad = false;
+__device__ __forceinline__ void mask_scores(f32x16 (&s)[NKB], LaneMask m, bool have_docs, uint32_t docs, int doc, int hh) {
 #pragma unroll
   for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      i32x4 id = {doc, doc, doc, doc};
-      if (have_docs) id = *(lds_i32x4*)(uintptr_t)(docs + (uint32_t)(32 * kb + 8 * g + 4 * hh) * 4u);
+    for (int i = 0; i < 16; ++i) s[kb][i] = m.dead(kb, i) ? -__builtin_inff() : s[kb][i];
+  if (have_docs)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * g + j;
-        const bool dead = m.dead(kb, i) || id[j] != doc;
-        s[kb][i] = dead ? -__builtin_inff() : s[kb][i];
-        if (bad != 0) sees_bad |= !dead && ((bad >> (key_of(kb, i) + 4 * hh)) & 1) != 0;
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const i32x4 id = *(lds_i32x4*)(uintptr_t)(docs + (uint32_t)(32 * kb + 8 * g + 4 * hh) * 4u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[kb][4 * g + j] = id[j] != doc ? -__builtin_inff() : s[kb][4 * g + j];
       }
-    }
-  return sees_bad;
+}
+
+// Whether this lane's row sees one of the keys whose bits are set.
+template <int NKB>
+__device__ __forceinline__ bool sees(const f32x16 (&s)[NKB], uint64_t keys, int hh) {
+  bool any = false;
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) any |= s[kb][i] != -__builtin_inff() && ((keys >> (key_of(kb, i) + 4 * hh)) & 1) != 0;
+  return any;
+}
+
+// Which half of its wavefront a lane is in; recomputed where it is needed.
+__device__ __forceinline__ int half_of(int tid) {
+  asm volatile("" : "+v"(tid));
+  return (tid >> 5) & 1;
 }
 
 // State of a lane's row.
@@ -186,6 +217,11 @@ __device__ __forceinline__ void masked_softmax(f32x16 (&s)[NKB], float mx, float
       }
       SCHED_FENCE();
     }
+  // Finished here, as in tile_softmax.
+#pragma unroll
+  for (int kb = 0; kb < NKB; ++kb)
+    asm volatile("" : "+v"(pb[kb][0]), "+v"(pb[kb][1]), "+v"(pb[kb][2]), "+v"(pb[kb][3]), "+v"(pb[kb][4]), "+v"(pb[kb][5]),
+                      "+v"(pb[kb][6]), "+v"(pb[kb][7]));
 }
 
 __device__ __forceinline__ bool pair_not_finite(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
@@ -234,6 +270,7 @@ __device__ __forceinline__ void add_not_finite(const MaskedParams& p, const char
           const int d = 32 * db + 8 * (i >> 2) + (i & 3) + 4 * hh;
           const uint32_t w = row[d >> 1], bits = d & 1 ? w & 0xFFFF0000u : w << 16;
           if (seen && (bits & 0x7F800000u) == 0x7F800000u) o[db][i] += __builtin_bit_cast(float, bits);
+          asm volatile("" : "+v"(o[db][i])::"memory");  // one at a time: this may not cost the tile loop registers
         }
     }
 }
@@ -246,7 +283,9 @@ constexpr int kDocsOff = T::ITEM_OFF + 16;
 template <class T>
 constexpr int kBadOff = kDocsOff<T> + 2 * T::BN * 4;
 template <class T>
-constexpr int kMaskedLds = kBadOff<T> + 3 * 8;
+constexpr int kRowDocsOff = kBadOff<T> + 3 * 8;
+template <class T>
+constexpr int kMaskedLds = kRowDocsOff<T> + T::BM * 4;
 
 // 64 ids -> LDS by one direct load of a dword a lane.
 __device__ __forceinline__ void lds_dma_4(const int32_t* base, uint32_t voff, uint32_t lds_addr) {
@@ -310,16 +349,133 @@ __device__ __forceinline__ void store_rows(const MaskedParams& p, const Lane<T>&
   }
 }
 
+// One step: the exponentials of tile t beside the MFMAs of S^T(t+1) = K(t+1) Q^T and of O^T += V(t)^T P(t)^T, in the slots of
+// tile_step (attn_device.h), then the maximum of S^T(t+1), with ABS also of its absolute values.
+//   POLY: the exponent of a score is sc * (poly[0] + .. sc^6) - mc: small raw scores of a cap are shaped here (see shape_scores).
+//   LSE: lx takes the sum of the fp32 probabilities.      issue: called behind every MFMA, for the loads of later tiles.
+template <class T, int KOFF, int VOFF, int PD, bool POLY, bool ABS, bool LSE, class Issue>
+__device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int (&ka_)[T::NKS], uint32_t (&pb)[T::NKB][8], const bf16x8 (&qf)[T::NKS],
+                                            f32x16 (&o)[T::NDB], f32x16 (&sc)[T::NKB], f32x16 (&sn)[T::NKB], float c, float mc,
+                                            const float (&poly)[4], float& mx, float& am, float& lx, Issue&& issue) {
+  using S = StepSlots<T>;
+  constexpr int NQ = T::NQK, N = S::N;
+  static_assert(T::NKB == 2, "two key blocks per tile");
+  bf16x8 frag[PD];
+  auto load_step = [&](auto jc) {
+    constexpr int J = decltype(jc)::value;
+    if constexpr (J >= NQ) {
+      constexpr int j = J - NQ, kb = j / (2 * T::NDB), u = (j / T::NDB) % 2, db = j % T::NDB;
+      lds_char* p0 = (lds_char*)(uintptr_t)(uint32_t)(va_[db] + VOFF + (32 * kb + 16 * u) * T::ROW_B);
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p0));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p0 + 8 * T::ROW_B));
+      frag[J % PD] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      constexpr int ks = J / T::NKB, kb = J % T::NKB;
+      frag[J % PD] = *(lds_bf16x8*)(uintptr_t)(uint32_t)(ka_[ks] + KOFF + kb * 32 * T::ROW_B);
+    }
+  };
+  auto mfma = [&](auto jc) {
+    constexpr int J = decltype(jc)::value;
+    if constexpr (J >= NQ) {
+      constexpr int j = J - NQ, kb = j / (2 * T::NDB), u = (j / T::NDB) % 2, db = j % T::NDB;
+      const u32x4 pw = {pb[kb][4 * u], pb[kb][4 * u + 1], pb[kb][4 * u + 2], pb[kb][4 * u + 3]};
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[J % PD], __builtin_bit_cast(bf16x8, pw), o[db], 0, 0, 0);
+    } else {
+      constexpr int ks = J / T::NKB, kb = J % T::NKB;
+      if constexpr (ks == 0) {
+        const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        sn[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[J % PD], qf[ks], zero, 0, 0, 0);
+      } else {
+        sn[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[J % PD], qf[ks], sn[kb], 0, 0, 0);
+      }
+    }
+  };
+  auto exponent = [&](float x) {
+    if constexpr (POLY) {
+      const float z = x * x;
+      return __builtin_fmaf(x, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, poly[3], poly[2]), poly[1]), poly[0]), -mc);
+    } else {
+      return __builtin_fmaf(x, c, -mc);
+    }
+  };
+  float e0 = 0.f, e1 = 0.f;  // a pair is packed behind the exponentials of the next one
+  auto unit = [&](auto kc) {
+    constexpr int k = decltype(kc)::value;
+    float f0 = 0.f, f1 = 0.f;
+    if constexpr (k < S::UNITS) {
+      constexpr int kb = k / 8, i = 2 * (k % 8);
+      f0 = __builtin_amdgcn_exp2f(exponent(sc[kb][i]));
+      f1 = __builtin_amdgcn_exp2f(exponent(sc[kb][i + 1]));
+    }
+    if constexpr (k > 0) {
+      SCHED_FENCE();
+      pb[(k - 1) / 8][(k - 1) % 8] = pack_bf16x2(e0, e1);
+      if constexpr (LSE) lx += e0 + e1;
+    }
+    e0 = f0;
+    e1 = f1;
+  };
+  SCHED_FENCE();
+  static_for<0, PD>([&](auto jc) { load_step(jc); });
+  SCHED_FENCE();
+  static_for<0, N>([&](auto jc) {
+    constexpr int J = decltype(jc)::value;
+    mfma(jc);
+    if constexpr (J + PD < N) load_step(IC<J + PD>{});
+    SCHED_FENCE();
+    static_for<S::first_unit(J), S::first_unit(J + 1)>(unit);
+    if constexpr (S::slot(S::UNITS - 1) == J) unit(IC<S::UNITS>{});
+    issue(jc);
+    if constexpr (J >= S::max_slot0) {
+      constexpr int m = J - S::max_slot0, kb = m / 2, i = 8 * (m % 2);
+#define DIT_MAX(out, first, open, close)                                                                                                    \
+  if constexpr (first)                                                                                                                      \
+    asm("v_max3_f32 %0, " open "%1" close ", " open "%2" close ", " open "%3" close "\n\tv_max3_f32 %0, %0, " open "%4" close ", " open   \
+        "%5" close "\n\tv_max3_f32 %0, %0, " open "%6" close ", " open "%7" close "\n\tv_max_f32 %0, %0, " open "%8" close               \
+        : "=&v"(out)                                                                                                                        \
+        : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),               \
+          "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]));                                                                                          \
+  else                                                                                                                                      \
+    asm("v_max3_f32 %0, %0, " open "%1" close ", " open "%2" close "\n\tv_max3_f32 %0, %0, " open "%3" close ", " open "%4" close         \
+        "\n\tv_max3_f32 %0, %0, " open "%5" close ", " open "%6" close "\n\tv_max3_f32 %0, %0, " open "%7" close ", " open "%8" close    \
+        : "+v"(out)                                                                                                                         \
+        : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),               \
+          "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]))
+      DIT_MAX(mx, m == 0, "", "");
+      if constexpr (ABS) {
+        DIT_MAX(am, m == 0, "|", "|");
+      }
+#undef DIT_MAX
+    }
+    SCHED_FENCE();
+  });
+  mx = max_with_other_half(mx);
+  SCHED_FENCE();
+}
+
+// The kernel works a tile ahead, as the unmasked 128-row kernel: the scores of the next tile are contracted beside the softmax of
+// this one.  What shapes and masks a tile's scores stands between two steps, for the tiles that need it.
+// Workgroups on a compute unit: what the registers allow.
+template <int D, bool CAP, bool LSE>
+constexpr int kMaskedWaves = D == 64 && !(CAP && LSE) ? 3 : 2;
+
 template <class T, bool CAP, bool BIAS, bool LSE>
-__global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu_waves_per_eu(2, 2))) masked_attn_kernel(MaskedParams p) {
+__global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu_waves_per_eu(kMaskedWaves<T::D, CAP, LSE>, kMaskedWaves<T::D, CAP, LSE>)))
+masked_attn_kernel(MaskedParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
   lds_char* smem = (lds_char*)smem_generic;
   const uint32_t lds = (uint32_t)(uintptr_t)smem;
   const int tid = threadIdx.x;
-  Lane<T> L;
-  L.init(tid, p.k_stride_b);
-  const uint32_t vvoff = (uint32_t)L.lrow * (uint32_t)p.v_stride_b + (uint32_t)L.vcol;
+  // Per-lane constants are recomputed where they are needed; kept live through the tile loop they are spilled.
+  auto fresh_lane = [&]() {
+    int x = tid;
+    asm volatile("" : "+v"(x));
+    Lane<T> l;
+    l.init(x, p.k_stride_b);
+    return l;
+  };
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // The item: heads fastest, so that with a multiple of eight heads an XCD keeps to its own ones; the last query tiles first,
   // which see the most keys under a causal mask.
@@ -347,13 +503,14 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu
     const int k = pos0 + row + 1 > sq.prefix ? pos0 + row + 1 : sq.prefix;
     return k < lim ? k : lim;
   };
-  int qrow = L.wave * 32 + L.l32;
-  const bool row_valid = qrow < it.q_rows;
-  if (!row_valid) qrow = it.q_rows - 1;
-  int klim = row_limit(qrow);
+  // This lane's query row, or the last one.
+  auto query_row = [&]() {
+    int x = tid;
+    asm volatile("" : "+v"(x));
+    const int row = (x >> 6) * 32 + (x & 31);
+    return row < it.q_rows ? row : it.q_rows - 1;
+  };
   const int klim_first = row_limit(0);
-  const int wave_last = L.wave * 32 + 31 < it.q_rows ? L.wave * 32 + 31 : it.q_rows - 1;
-  const int klim_wave = __builtin_amdgcn_readfirstlane(row_limit(wave_last));
 
   LiveTiles tiles;
   tiles.ranges = nullptr;
@@ -361,16 +518,15 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu
   tiles.live = tiles.pure = 0;
   const int nt = lim > 0 ? (lim + T::BN - 1) / T::BN : 0;
   const int64_t part_end = ((int64_t)it.part + 1) * p.part_tiles;
-  int t = nt;
-  if ((int64_t)it.part * p.part_tiles < nt) t = it.part * p.part_tiles;
+  int t0 = nt;
+  if ((int64_t)it.part * p.part_tiles < nt) t0 = it.part * p.part_tiles;
   tiles.end = part_end < nt ? (int)part_end : nt;
   const bool have_docs = p.q_doc != nullptr;
-  int doc = 0;
   const int32_t* kdoc = nullptr;
   if (have_docs) {
     kdoc = p.k_doc + sq.kv_start;
-    doc = p.q_doc[it.q_start + qrow];
-    if (doc < 0) klim = 0;  // sees nothing
+    const int row = query_row();  // a row's id is read back by the wavefront that wrote it
+    *(lds_u32*)(uintptr_t)(lds + kRowDocsOff<T> + row * 4) = (uint32_t)p.q_doc[it.q_start + row];
     const DocTile a = doc_range(p.q_doc + it.q_start, it.q_rows < 64 ? it.q_rows : 64);
     const DocTile b = it.q_rows > 64 ? doc_range(p.q_doc + it.q_start + 64, it.q_rows - 64) : a;
     tiles.mine.lo = a.lo < b.lo ? a.lo : b.lo;
@@ -378,7 +534,13 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu
     tiles.mine.any_lo = a.any_lo < b.any_lo ? a.any_lo : b.any_lo;
     tiles.ranges = p.doc_tiles + sq.tile0;
   }
-  t = tiles.next(t);
+  t0 = tiles.next(t0);
+
+  // The id of this lane's row, and the keys that the row sees are under the limit.
+  auto row_mask = [&](int row, int& doc) {
+    doc = have_docs ? (int)*(lds_u32*)(uintptr_t)(lds + kRowDocsOff<T> + row * 4) : 0;
+    return doc < 0 ? 0 : row_limit(row);
+  };
 
   f32x16 o[T::NDB];
 #pragma unroll
@@ -386,98 +548,265 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   RowState r = {kNoReference, 0.f, 0.f};
-  bool poison = false;
 
-  if (t < tiles.end) {
+  if (t0 < tiles.end) {
     const int kv_head = it.head / p.group;
     const char* kbase = static_cast<const char*>(p.k) + (int64_t)it.kv_start * p.k_stride_b + (int64_t)kv_head * T::ROW_B;
     const char* vbase = static_cast<const char*>(p.v) + (int64_t)it.kv_start * p.v_stride_b + (int64_t)kv_head * T::ROW_B;
-    const float c = CAP || BIAS ? 1.f : p.c_log2;
     const float slope = BIAS ? p.slopes[it.head] * 1.44269504088896340736f : 0.f;
-
-    auto load = [&](int ti, int slot) {
-      const int key0 = tile_first_key<T>(ti, lim);
-      tile_load_one<T>(kbase, p.k_stride_b, key0, lim, L.lrow, L.kcol, L.kvoff, smem, T::K_OFF + slot * T::TILE_B, L.wave);
-      tile_load_one<T>(vbase, p.v_stride_b, key0, lim, L.lrow, L.vcol, vvoff, smem, T::V_OFF + slot * T::TILE_B, L.wave);
-      if (have_docs && L.wave == 0) {
-        const int last = lim - 1 - key0;
-        lds_dma_4(kdoc + key0, (uint32_t)(L.lane < last ? L.lane : last) * 4u, lds + kDocsOff<T> + slot * (T::BN * 4));
-      }
+    const uint32_t lds_wave = lds + (uint32_t)wave * 1024u;
+    const TailRows tail = tail_rows<T>(lim);
+    uint32_t kvoff, vvoff;
+    {
+      const Lane<T> L = fresh_lane();
+      kvoff = L.kvoff;
+      vvoff = (uint32_t)L.lrow * (uint32_t)p.v_stride_b + (uint32_t)L.vcol;
+    }
+    // Some pair of a row of the item and a key of tile t is dead.  Asked before the walk over the tiles goes on.
+    auto needs_mask = [&](int t) {
+      return (t == nt - 1 && tail.hi - tail.lo != T::BN) || klim_first < tile_first_key<T>(t, lim) + T::BN || !tiles.is_pure(t);
     };
-    const uint32_t spare = lds + (L.wave < 2 ? T::K_OFF : T::V_OFF) + T::TILE_B + (uint32_t)(L.wave % 2) * (32 * T::ROW_B);
+    // Whole tiles (keys under a tile are loaded as a tile of the last 64 ones, or, where all of them are under one, in the prologue).
+    auto load_k = [&](int t, int slot) {
+      const int key0 = tile_first_key<T>(t, lim);
+      const char* base = kbase + (int64_t)key0 * p.k_stride_b;
+#pragma unroll
+      for (int i = 0; i < T::LPT; ++i)
+        lds_dma_16(base + (int64_t)(i * T::GROUP) * p.k_stride_b, kvoff, lds_wave + T::K_OFF + slot * T::TILE_B + i * T::NWAVES * 1024);
+      if (have_docs && wave == 0) lds_dma_4(kdoc + key0, (uint32_t)(tid * 4), lds + kDocsOff<T> + slot * (T::BN * 4));
+    };
+    auto load_v = [&](int t, int slot) {
+      const char* base = vbase + (int64_t)tile_first_key<T>(t, lim) * p.v_stride_b;
+#pragma unroll
+      for (int i = 0; i < T::LPT; ++i)
+        lds_dma_16(base + (int64_t)(i * T::GROUP) * p.v_stride_b, vvoff, lds_wave + T::V_OFF + slot * T::TILE_B + i * T::NWAVES * 1024);
+    };
+
+    // Q goes through slots that the first tiles do not need yet.
+    const uint32_t spare = lds + (wave < 2 ? T::K_OFF : T::V_OFF) + T::TILE_B + (uint32_t)(wave % 2) * (32 * T::ROW_B);
     static_assert(T::TILE_B == 2 * 32 * T::ROW_B, "two wavefronts' rows in a tile");
-    q_rows_load<T>(p, L, it, p.q_stride_b, (int64_t)it.head * T::ROW_B, spare);
-    load(t, 0);
+    bool masked0 = needs_mask(t0);
+    {
+      const Lane<T> L = fresh_lane();
+      q_rows_load<T>(p, L, it, p.q_stride_b, (int64_t)it.head * T::ROW_B, spare);
+      if (lim >= T::BN) {
+        load_k(t0, 0);
+        load_v(t0, 0);
+      } else {
+        tile_load_one<T>(kbase, p.k_stride_b, 0, lim, L.lrow, L.kcol, kvoff, smem, T::K_OFF, wave);
+        if (have_docs && wave == 0) lds_dma_4(kdoc, (uint32_t)(tid < lim ? tid : lim - 1) * 4u, lds + kDocsOff<T>);
+        tile_load_one<T>(vbase, p.v_stride_b, 0, lim, L.lrow, L.vcol, vvoff, smem, T::V_OFF, wave);
+      }
+    }
     if (tid < 6) *(lds_u32*)(uintptr_t)(lds + kBadOff<T> + tid * 4) = 0;
-    wait_loads();
+    int t1 = tiles.next(t0 + 1);
+    bool masked1 = t1 < tiles.end && needs_mask(t1);
+    int t2 = tiles.next(t1 + 1);
+    bool masked2 = t2 < tiles.end && needs_mask(t2);
+    wait_loads_but<T::LPT>();  // V is awaited before its step
     bf16x8 qf[T::NKS];
-    q_rows_read<T>(p, L, spare, qf);
+    q_rows_read<T>(p, fresh_lane(), spare, qf);
     wg_barrier();
     int ka[T::NKS], va[T::NDB];
-    L.operand_addrs(lds, lds, ka, va);
-    int slot = 0, turn = 0;  // of the K / V buffers and of the bad-key masks
-    const TailRows tail = tail_rows<T>(lim);
+    fresh_lane().operand_addrs(lds, lds, ka, va);
+    int turn = 0;  // of the bad-key masks
+    bool poison = false;
+    float mx = 0.f, am = 0.f;
+    f32x16 sa[T::NKB], sb[T::NKB];
+    uint32_t pb[T::NKB][8];
+    const float c = CAP || BIAS ? 1.f : p.c_log2;
 
-    while (t < tiles.end) {
+    // Scores of tile t, from S^T to base-2 exponents with the dead ones -inf, and their maximum mx.  Before, mx (and am) are
+    // those of the raw scores; the cap is monotonic, so the capped maximum is that of the raw one.
+    auto is_small = [&]() { return CAP && __builtin_amdgcn_ballot_w64(am > p.small) == 0; };
+    auto finish = [&](f32x16(&s)[T::NKB], int t, int slot, bool masked) {
       const int key0 = tile_first_key<T>(t, lim);
-      const bool last = t == nt - 1;
-      const int lo = last ? tail.lo : 0;
-      // Some pair of a row of the item and a key of the tile is dead.
-      const bool masked = (last && tail.hi - tail.lo != T::BN) || klim_first < key0 + T::BN || !tiles.is_pure(t);
-      const int tn = tiles.next(t + 1);
-      wait_loads();
-      const uint32_t bad_at = lds + kBadOff<T> + (uint32_t)turn * 8u;
+      if constexpr (CAP || BIAS)
+        shape_scores<T::NKB, CAP, BIAS>(s, p, is_small(), slope, BIAS ? pos0 + query_row() - key0 - 4 * half_of(tid) : 0);
       if (masked) {
-        const uint32_t found = make_finite<T::LPT>(lds + T::V_OFF + slot * T::TILE_B + L.wave * 1024 + L.lane * 16, T::NWAVES * 1024);
-        if (found != 0) {
-#pragma unroll
-          for (int i = 0; i < T::LPT; ++i) {
-            const int row = i * T::GROUP + L.lrow;
-            if (found >> i & 1) __hip_atomic_fetch_or((lds_u32*)(uintptr_t)(bad_at + (uint32_t)(row >> 5) * 4u), 1u << (row & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-          }
-        }
+        int doc;
+        const int hh = half_of(tid), klim = row_mask(query_row(), doc);
+        const int lo = t == nt - 1 ? tail.lo : 0, n = klim - key0 - lo;
+        const LaneMask m = {lo - 4 * hh, n > 0 ? (unsigned)n : 0u};
+        mask_scores<T::NKB>(s, m, have_docs, lds + kDocsOff<T> + slot * (T::BN * 4), doc, hh);
       }
-      wg_barrier();
-      if (tn < tiles.end) load(tn, slot ^ 1);
-      if (tid < 2) *(lds_u32*)(uintptr_t)(lds + kBadOff<T> + (uint32_t)(turn == 0 ? 2 : turn - 1) * 8u + tid * 4) = 0;
-      if (key0 + lo < klim_wave) {  // a wavefront none of whose rows sees the tile skips it
-        f32x16 s[T::NKB];
-        uint32_t pb[T::NKB][8];
-        mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, s);
-        if constexpr (CAP || BIAS) shape_scores<T::NKB, CAP, BIAS>(s, p, slope, pos0 + qrow - key0 - 4 * L.hh);
-        if (masked) {
-          const int n = klim - key0 - lo;
-          const LaneMask m = {lo - 4 * L.hh, n > 0 ? (unsigned)n : 0u};
-          const uint64_t bad = (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)bad_at) |
-                               (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)(bad_at + 4)) << 32;
-          poison |= mask_scores<T::NKB>(s, m, have_docs, lds + kDocsOff<T> + slot * (T::BN * 4), doc, L.hh, bad);
-        }
+      if (BIAS || masked) {
         scores_ready<T>(s);
-        const float mx = tile_max<T>(s);
-        masked_softmax<T::NKB, T::NDB, LSE>(s, mx, c, pb, o, r);
-        mfma_stream<T, true, 0, 0, kPrefetch>(smem, va, ka, pb, qf, o, s);
-        r.l += row_sum<T>(pb);
+        mx = tile_max<T>(s);
+      } else if constexpr (CAP) {
+        mx = capped(p, mx);
       }
+    };
+    // Behind the loads of V of a masked tile, before the barrier: this wavefront's rows of it become finite.
+    auto clean_v = [&](int slot) {
+      const uint32_t found = make_finite<T::LPT>(lds_wave + T::V_OFF + slot * T::TILE_B + (tid & 63) * 16, T::NWAVES * 1024);
+      if (found != 0) {
+        const int lrow = fresh_lane().lrow;
 #pragma unroll
-      for (int ks = 0; ks < T::NKS; ++ks) ka[ks] ^= T::TILE_B;
+        for (int i = 0; i < T::LPT; ++i) {
+          const int row = i * T::GROUP + lrow;
+          if (found >> i & 1)
+            __hip_atomic_fetch_or((lds_u32*)(uintptr_t)(lds + kBadOff<T> + (uint32_t)turn * 8u + (uint32_t)(row >> 5) * 4u), 1u << (row & 31),
+                                  __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+      }
+    };
+    // Behind that barrier: whether a row of this lane sees one of those keys.  Clears the mask of the tile after the next.
+    auto look_bad = [&](const f32x16(&s)[T::NKB], bool masked) {
+      if (masked) {
+        const uint32_t at = lds + kBadOff<T> + (uint32_t)turn * 8u;
+        const uint64_t bad = (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)at) |
+                             (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)(at + 4)) << 32;
+        if (bad != 0) poison |= sees<T::NKB>(s, bad, half_of(tid));
+      }
+      const int clear = turn == 0 ? 2 : turn - 1;
+      if (tid < 2) *(lds_u32*)(uintptr_t)(lds + kBadOff<T> + (uint32_t)clear * 8u + tid * 4) = 0;
+      turn = turn == 2 ? 0 : turn + 1;
+    };
+    auto raise = [&]() {
+      const bool grow = (mx - r.m_ref) * c > kRescaleLog2;
+      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+        const float m_new = grow ? mx : r.m_ref;
+        const float alpha = __builtin_amdgcn_exp2f((r.m_ref - m_new) * c);
+        r.m_ref = m_new;
+        r.l *= alpha;
+        if constexpr (LSE) r.lx *= alpha;
+#pragma unroll
+        for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+      }
+    };
+
+    if (t1 < tiles.end) load_k(t1, 1);
+    mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, sa);
+    scores_ready<T>(sa);
+    mx = tile_max<T>(sa);
+    am = __builtin_inff();  // the first tile's cap is not the polynomial
+
+    // Tiles under free_end need no mask but for ids.  In a run of such tiles, whose ids agree too, a step has no tests and loads
+    // from running pointers, spread behind its MFMAs.
+    const int free_end = klim_first / T::BN < tiles.end ? klim_first / T::BN : tiles.end;
+    constexpr int NLOAD = 2 * T::LPT, EVERY = (T::NQK + T::NPV) / 2 / NLOAD;
+    static_assert(EVERY >= 1, "a step's loads fit its slots");
+    const char *kp = kbase, *vp = vbase;
+    const int64_t k_step = (int64_t)T::BN * p.k_stride_b, v_step = (int64_t)T::BN * p.v_stride_b;
+    // A step from t (scores raw with POLY, else finished, in sc; K(t + 1) and V(t) on their way) to t + 1 (raw, in sn).
+    auto run_step = [&](auto uc, f32x16(&sc)[T::NKB], f32x16(&sn)[T::NKB]) {
+      constexpr int U = decltype(uc)::value;
+      constexpr bool POLY = CAP && !BIAS;
+      wait_loads();
+      wg_barrier();
+      float poly[4] = {1.f, 0.f, 0.f, 0.f};
+      if constexpr (POLY) {
+        mx = capped(p, mx);
+        if (is_small()) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) poly[i] = p.poly[i];
+        } else {
+          shape_scores<T::NKB, CAP, false>(sc, p, false, 0.f, 0);
+        }
+      }
+      raise();
+      const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
+      masked_step<T, (1 - U) * T::TILE_B, U * T::TILE_B, kPrefetch, POLY, CAP, LSE>(
+          va, ka, pb, qf, o, sc, sn, c, mc, poly, mx, am, r.lx, [&](auto jc) {
+            constexpr int J = decltype(jc)::value;
+            if constexpr (J % EVERY == EVERY / 2 && J / EVERY < NLOAD) {
+              constexpr int j = J / EVERY, i = j % T::LPT;
+              if constexpr (j < T::LPT)
+                lds_dma_16_at<T::K_OFF + U * T::TILE_B + i * T::NWAVES * 1024>(kp + (int64_t)(i * T::GROUP) * p.k_stride_b, kvoff, lds_wave);
+              else
+                lds_dma_16_at<T::V_OFF + (1 - U) * T::TILE_B + i * T::NWAVES * 1024>(vp + (int64_t)(i * T::GROUP) * p.v_stride_b, vvoff, lds_wave);
+            }
+          });
+      kp += k_step;
+      vp += v_step;
+      r.l += row_sum<T>(pb);
+      asm volatile("" : "+v"(r.l));
+      ++t0;
+    };
+    int slot = 0;  // of K(t0) and V(t0); ka and va point there
+    auto turn_slots = [&]() {
 #pragma unroll
       for (int db = 0; db < T::NDB; ++db) va[db] ^= T::TILE_B;
       slot ^= 1;
-      turn = turn == 2 ? 0 : turn + 1;
-      t = tn;
+    };
+    auto turn_k = [&]() {
+#pragma unroll
+      for (int ks = 0; ks < T::NKS; ++ks) ka[ks] ^= T::TILE_B;
+    };
+    while (t1 < tiles.end) {
+      // Here the scores of t0 are raw, in sa; K(t1) and V(t0) are on their way.
+      if (slot == 0 && !masked0) {
+        int run_end = free_end;
+        if (tiles.ranges != nullptr) {
+          const int rest = t0 >= tiles.base ? t0 + (int)__builtin_ctzll(~((tiles.live & tiles.pure) >> (t0 - tiles.base)) | 1ull << 63) : t0;
+          run_end = rest < run_end ? rest : run_end;
+        }
+        if (t0 + 3 < run_end) {
+          kp = kbase + (int64_t)(t0 + 2) * k_step;
+          vp = vbase + (int64_t)(t0 + 1) * v_step;
+          do {
+            if constexpr (BIAS) finish(sa, t0, 0, false);
+            run_step(IC<0>{}, sa, sb);
+            if constexpr (BIAS) finish(sb, t0, 0, false);
+            run_step(IC<1>{}, sb, sa);
+          } while (t0 + 3 < run_end);
+          t1 = t0 + 1;
+          t2 = tiles.next(t1 + 1);
+          masked0 = masked1 = false;
+          masked2 = t2 < tiles.end && needs_mask(t2);
+        }
+      }
+      finish(sa, t0, slot, masked0);
+      const int t3 = tiles.next(t2 + 1);
+      const bool masked3 = t3 < tiles.end && needs_mask(t3);
+      wait_loads();
+      if (masked0) clean_v(slot);
+      wg_barrier();
+      if (t2 < tiles.end) load_k(t2, slot);
+      load_v(t1, slot ^ 1);
+      look_bad(sa, masked0);
+      raise();
+      const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
+      turn_k();
+      masked_step<T, 0, 0, kPrefetch, false, CAP, LSE>(va, ka, pb, qf, o, sa, sb, c, mc, p.poly, mx, am, r.lx, [](auto) {});
+      turn_slots();
+      r.l += row_sum<T>(pb);
+      asm volatile("" : "+v"(r.l));
+#pragma unroll
+      for (int kb = 0; kb < T::NKB; ++kb) sa[kb] = sb[kb];
+      t0 = t1;
+      t1 = t2;
+      t2 = t3;
+      masked0 = masked1;
+      masked1 = masked2;
+      masked2 = masked3;
     }
+    finish(sa, t0, slot, masked0);
+    wait_loads();
+    if (masked0) clean_v(slot);
+    wg_barrier();
+    look_bad(sa, masked0);
+    masked_softmax<T::NKB, T::NDB, LSE>(sa, mx, c, pb, o, r);
+    mfma_stream<T, true, 0, 0, kPrefetch>(smem, va, ka, pb, qf, o, sa);
+    r.l += row_sum<T>(pb);
     if (__builtin_amdgcn_ballot_w64(poison) != 0) {
       const int k0 = it.part * p.part_tiles * T::BN;
-      add_not_finite<T>(p, vbase, kdoc, k0, tiles.end * T::BN < lim ? tiles.end * T::BN : lim, T::BN, T::BN, klim, doc, L.hh, o);
+      int doc;
+      const int klim = row_mask(query_row(), doc);
+      add_not_finite<T>(p, vbase, kdoc, k0, tiles.end * T::BN < lim ? tiles.end * T::BN : lim, T::BN, T::BN, klim, doc, half_of(tid), o);
     }
-    wg_barrier();  // the rows are staged in the K buffers
+    // The rows are staged in the K buffers, which nobody reads behind the last barrier.
   }
 
   const float l = r.l + __shfl_xor(r.l, 32), lx = r.lx + __shfl_xor(r.lx, 32);
   const bool any = l > 0.f || l != l;
-  store_rows<T>(p, L, it, o, any ? 1.f / l : 0.f, lds + T::K_OFF + (uint32_t)L.wave * (32 * T::ROW_B));
+  store_rows<T>(p, fresh_lane(), it, o, any ? 1.f / l : 0.f, lds + T::K_OFF + (uint32_t)wave * (32 * T::ROW_B));
   if constexpr (LSE) {
-    if (row_valid && L.hh == 0) {
+    const int qrow = wave * 32 + (tid & 31);
+    if (qrow < it.q_rows && (tid & 32) == 0) {
       const float c = CAP || BIAS ? 1.f : p.c_log2;
       float* dst = p.part_out != nullptr ? p.part_lse + (int64_t)it.part * p.part_rows * n_heads : p.lse;
       dst[(int64_t)(it.q_start + qrow) * n_heads + it.head] = any ? kLn2 * (r.m_ref * c + __builtin_amdgcn_logf(lx)) : -__builtin_inff();
@@ -653,11 +982,12 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
       f32x16 s[1];
       uint32_t pb[1][8];
       mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, s);
-      if constexpr (CAP || BIAS) shape_scores<1, CAP, BIAS>(s, p, slope, pos0 + row - key0 - 4 * hh);
+      if constexpr (CAP || BIAS) shape_scores<1, CAP, BIAS>(s, p, false, slope, pos0 + row - key0 - 4 * hh);
       if (masked) {
         const int n = klim - key0;
         const LaneMask m = {-4 * hh, n > 0 ? (unsigned)n : 0u};
-        poison |= mask_scores<1>(s, m, have_docs, docs + (uint32_t)stage * 128u, doc, hh, bad);
+        mask_scores<1>(s, m, have_docs, docs + (uint32_t)stage * 128u, doc, hh);
+        if (bad != 0) poison |= sees<1>(s, bad, hh);
       }
       asm volatile("s_nop 11" : "+v"(s[0]));  // as scores_ready
       const float mx = tile_max<T>(s);
