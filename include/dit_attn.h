@@ -284,8 +284,8 @@ int dit_attn_qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const
  * effect on it.  So a padded batch gives its padding rows negative ids, several documents of a sequence get an id each (in any
  * order), and text that all of an ordered sequence sees is its prefix.
  *   q           DEVICE bf16 [Tq, n_heads, head_dim];  k, v  DEVICE bf16 [Tk, n_kv_heads, head_dim];  16-byte aligned.
- *   row_strides HOST, elements from row to row of q, k and v (multiples of 8, at most 2^24), or NULL: contiguous.  The heads of a
- *               row are contiguous.
+ *   row_strides HOST, elements from row to row of q, k and v (multiples of 8, at most 2^24; 0: contiguous), or NULL: contiguous.
+ *               The heads of a row are contiguous.
  *   cu_seqlens_q, cu_seqlens_k   HOST, as dit_attn_cross_varlen_fwd; cu_seqlens_k may be NULL: keys share the query boundaries.
  *               Any number of sequences.
  *   n_kv_heads  divides n_heads.      head_dim  64 or 128.      scale  finite.

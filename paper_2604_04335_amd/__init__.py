@@ -234,14 +234,20 @@ def _ptr(x) -> int:
     return int(x)
 
 
+_I64x3 = ctypes.c_int64 * 3
+
+
 def _row_stride(x, name: str) -> int:
-    """Elements from row to row of a bf16 tensor [rows, heads, head_dim] with contiguous heads; 0 (contiguous) for an address."""
+    """Elements from row to row of a bf16 tensor [rows, heads, head_dim] with contiguous heads; 0: contiguous, or an address."""
     if not hasattr(x, "stride"):
         return 0
-    shape, (rows, heads, inner) = x.shape, x.stride()
-    if x.element_size() != 2 or (inner != 1 and shape[2] > 1) or (heads != shape[2] and shape[1] > 1):
-        raise ValueError(f"{name}: a bf16 tensor [rows, heads, head_dim] whose heads are contiguous")
-    return rows if shape[0] > 1 else shape[1] * shape[2]
+    if x.element_size() == 2:
+        if x.is_contiguous():
+            return 0
+        shape, (rows, heads, inner) = x.shape, x.stride()
+        if (inner == 1 or shape[2] == 1) and (heads == shape[2] or shape[1] == 1):
+            return rows if shape[0] > 1 else 0
+    raise ValueError(f"{name}: a bf16 tensor [rows, heads, head_dim] whose heads are contiguous")
 
 
 def _cu_array(cu_seqlens) -> np.ndarray:
@@ -428,7 +434,7 @@ def dit_attn_masked_varlen_fwd(ctx, q, k, v, cu_seqlens_q, cu_seqlens_k, n_heads
     """Attention with masks, capped scores and a distance bias; see include/dit_attn.h.
 
     q, k, v: bf16 tensors [rows, heads, head_dim] whose rows may be strided, or integer addresses (with row_strides, three
-    numbers of elements, unless contiguous).  cu_seqlens_k may be None (that of the queries); mask, lse may be None.
+    numbers of elements, 0: contiguous).  cu_seqlens_k may be None (that of the queries); mask, lse may be None.
     """
     lib = load_library()
     cq = _cu_array(cu_seqlens_q)
@@ -439,12 +445,10 @@ def dit_attn_masked_varlen_fwd(ctx, q, k, v, cu_seqlens_q, cu_seqlens_k, n_heads
         raise ValueError("cu_seqlens_q and cu_seqlens_k need n_seqs + 1 entries")
     if mask is not None and mask.n_prefix is not None and mask.n_prefix < n_seqs:
         raise ValueError("mask.prefix needs an entry for every sequence")
-    if row_strides is None and hasattr(q, "stride"):
+    if row_strides is None:
         row_strides = (_row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v"))
-    if row_strides is not None:
-        row_strides = (ctypes.c_int64 * 3)(*row_strides)
-    rc = lib.dit_attn_masked_varlen_fwd(ctx, _ptr(q), _ptr(k), _ptr(v), row_strides, cq.ctypes.data, None if ck is None else ck.ctypes.data,
-                                        n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, _ptr(out), _ptr(lse), _ptr(stream))
+    rc = lib.dit_attn_masked_varlen_fwd(ctx, _ptr(q), _ptr(k), _ptr(v), _I64x3(*row_strides), cq.__array_interface__["data"][0],
+                                        None if ck is None else ck.__array_interface__["data"][0], n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, _ptr(out), _ptr(lse), _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 

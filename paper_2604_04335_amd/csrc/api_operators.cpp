@@ -6,7 +6,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <numeric>
 #include <string>
 #include <vector>
 
@@ -85,9 +84,9 @@ int rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_rows, cons
   int pair = 0;
   for (int a = 0; a < r->n_axes; ++a)
     for (int j = 0; j < r->axis_dim[a] / 2; ++j, ++pair) {
-      const long double turns = static_cast<long double>(rope_frequency(*r, a, j)) / 6.283185307179586476925286766559L;
-      p.turns_hi[pair] = static_cast<double>(turns);
-      p.turns_lo[pair] = static_cast<double>(turns - static_cast<long double>(p.turns_hi[pair]));
+      const long double quarters = static_cast<long double>(rope_frequency(*r, a, j)) / 1.5707963267948966192313216916398L;
+      p.quarters_hi[pair] = static_cast<double>(quarters);
+      p.quarters_lo[pair] = static_cast<double>(quarters - static_cast<long double>(p.quarters_hi[pair]));
       p.axis[pair] = static_cast<uint8_t>(a);
     }
   dit::DeviceGuard guard;
@@ -164,16 +163,47 @@ int qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const dit_attn
 
 int64_t tiles_of(int64_t keys) { return (keys + 63) / 64; }
 
-// Parts that the keys of every sequence are split into, and the tiles of a part.
-// Few rows: a workgroup (160 KB of LDS, so one on a compute unit) for each of them, at least four tiles each.
-// Else: where the items leave half of the workgroups' places idle, parts of at least sixteen tiles.
-void choose_parts(int64_t items, int64_t max_tiles, bool few_rows, int n_cus, int32_t* n_parts, int32_t* part_tiles) {
-  const int64_t places = few_rows ? n_cus : 2 * static_cast<int64_t>(n_cus);
-  int64_t n = std::min<int64_t>({places / std::max<int64_t>(items, 1), max_tiles / (few_rows ? 4 : 16), dit::kMaskedMaxParts});
-  n = std::max<int64_t>(n, 1);
-  const int64_t per = std::max<int64_t>((max_tiles + n - 1) / n, 1);
-  *part_tiles = static_cast<int32_t>(per);
-  *n_parts = static_cast<int32_t>(std::max<int64_t>((max_tiles + per - 1) / per, 1));
+// Tiles of a part: the keys of a sequence are split into parts of so many 64-key tiles, as few as still make no more work items
+// than there are compute units (two to each where parts have 32 tiles even so), or not at all where that is no quicker.
+// Measured on MI355X, us:
+//   one item to a compute unit or two  512 x 4 heads against 40000 keys (head dimension 64) 34.6 / 42.8, 1570 x 5 20.8 / 27.0, 4951 x
+//     3 50.2 / 51.0;  226 rows x 24 heads against 20506 keys 90 / 94 on the same keys over and over, 107 / 101 on changing ones: a
+//     workgroup by itself waits for its tiles to come from HBM;  parts of at least 6 tiles or 16  77 x 24 against 4352 20.5 / 24.3.
+//   unsplit / split, the unsplit call taking 0.65 us a tile (few rows 0.33, at head dimension 64 0.19), the join 4 us and the
+//     partial results 0.33 us a megabyte:  1024 x 8 17.1 / 19.0, 2048 x 4 28.0 / 24.6, 33 x 8 against 1024 17.0 / 14.4, 410 x 24
+//     (64) 9.6 / 14.5;  one row of 8 heads against 768 keys 8.8 / 9.7, 1024 10.1 / 9.9, 2048 15.6 / 9.5, 20506 131 / 22.5;  at head
+//     dimension 64, 24 heads, 1024 7.5 / 8.6, 1536 9.1 / 9.2, 2048 10.6 / 8.1.
+// Few rows: parts of at least 4 tiles (2 to 8: level).
+struct SeqWork {
+  int64_t items, tiles, rows;  // items unsplit, key tiles, query rows
+};
+int64_t parts_of(int64_t tiles, int64_t part_tiles) { return std::max<int64_t>((tiles + part_tiles - 1) / part_tiles, 1); }
+
+int64_t choose_part_tiles(const std::vector<SeqWork>& seqs, bool few_rows, int32_t n_heads, int32_t head_dim, int n_cus) {
+  int64_t max_tiles = 1;
+  for (const SeqWork& s : seqs) max_tiles = std::max(max_tiles, s.tiles);
+  const int64_t least = std::max<int64_t>(few_rows ? 4 : 6, (max_tiles + dit::kMaskedMaxParts - 1) / dit::kMaskedMaxParts);
+  const auto fit = [&](int64_t places) {
+    int64_t lo = least, hi = std::max(max_tiles, least);
+    while (lo < hi) {  // the least of [lo, hi] that fits; hi splits nothing
+      const int64_t mid = (lo + hi) / 2;
+      int64_t n = 0;
+      for (const SeqWork& s : seqs) n += s.items * parts_of(s.tiles, mid);
+      if (n <= places) hi = mid;
+      else lo = mid + 1;
+    }
+    return lo;
+  };
+  int64_t lo = fit(n_cus);
+  if (!few_rows && lo >= 32) {
+    const int64_t two = fit(2 * static_cast<int64_t>(n_cus));
+    if (two >= 32) lo = two;
+  }
+  double part_mb = 0;
+  for (const SeqWork& s : seqs)
+    if (s.tiles > lo) part_mb += static_cast<double>(s.rows * parts_of(s.tiles, lo)) * n_heads * head_dim * 4e-6;
+  const double tile_us = !few_rows ? 0.65 : head_dim == 64 ? 0.19 : 0.33;
+  return tile_us * static_cast<double>(max_tiles - lo) > 4.0 + 0.33 * part_mb ? lo : max_tiles;
 }
 
 int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* v, const int64_t* row_strides, const int32_t* cu_q,
@@ -196,12 +226,13 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
     for (int32_t i = 0; i < n_seqs; ++i)
       if (m.prefix[i] < 0) return fail(ctx, DIT_ATTN_ERR_MASK, "prefix must not be negative");
   if ((m.q_doc == nullptr) != (m.k_doc == nullptr)) return fail(ctx, DIT_ATTN_ERR_MASK, "q_doc and k_doc come together");
-  const int64_t dense[3] = {static_cast<int64_t>(n_heads) * head_dim, static_cast<int64_t>(n_kv_heads) * head_dim,
-                            static_cast<int64_t>(n_kv_heads) * head_dim};
-  const int64_t* strides = row_strides ? row_strides : dense;
-  for (int i = 0; i < 3; ++i)
-    if (strides[i] < dense[i] || strides[i] % 8 != 0 || strides[i] > (int64_t{1} << 24))
+  int64_t strides[3];
+  for (int i = 0; i < 3; ++i) {
+    const int64_t row = static_cast<int64_t>(i == 0 ? n_heads : n_kv_heads) * head_dim;
+    strides[i] = row_strides && row_strides[i] != 0 ? row_strides[i] : row;
+    if (strides[i] < row || strides[i] % 8 != 0 || strides[i] > (int64_t{1} << 24))
       return fail(ctx, DIT_ATTN_ERR_STRIDE, "row strides must be multiples of 8 elements, hold a row's heads and be at most 2^24");
+  }
   const int64_t total_q = n_seqs > 0 ? cu_q[n_seqs] : 0, total_k = n_seqs > 0 ? cu_k[n_seqs] : 0;
   if (total_q == 0) return DIT_ATTN_OK;
   if (!q || !out || (total_k > 0 && (!k || !v))) return fail(ctx, DIT_ATTN_ERR_NULL, "q, k, v and out must be non-NULL");
@@ -212,24 +243,32 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
 
   // Sequences with query rows, the most keys first: their items take longest.
   std::vector<int32_t> order;
-  int64_t max_rows = 0, items = 0, max_tiles = 0, total_tiles = 0;
+  int64_t max_rows = 0, total_tiles = 0;
   const int32_t group = n_heads / n_kv_heads;
   for (int32_t i = 0; i < n_seqs; ++i) {
-    const int64_t lq = cu_q[i + 1] - cu_q[i], lk = cu_k[i + 1] - cu_k[i];
+    const int64_t lq = cu_q[i + 1] - cu_q[i], tiles = tiles_of(cu_k[i + 1] - cu_k[i]);
     if (lq == 0) continue;
     order.push_back(i);
     max_rows = std::max(max_rows, lq);
-    max_tiles = std::max(max_tiles, tiles_of(lk));
-    total_tiles += tiles_of(lk);
-    items += (lq + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads;
+    total_tiles += tiles;
   }
   std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cu_k[a + 1] - cu_k[a] > cu_k[b + 1] - cu_k[b]; });
   const bool few_rows = max_rows * group <= dit::kMaskedFewRows;
-  if (few_rows) items = static_cast<int64_t>(order.size()) * n_kv_heads;
-
+  std::vector<SeqWork> seqs;
+  for (const int32_t i : order) {
+    const int64_t lq = cu_q[i + 1] - cu_q[i];
+    seqs.push_back({few_rows ? n_kv_heads : (lq + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads, tiles_of(cu_k[i + 1] - cu_k[i]), lq});
+  }
   dit::MaskedParams p{};
-  choose_parts(items, max_tiles, few_rows, ctx->n_cus, &p.n_parts, &p.part_tiles);
-  if (items * p.n_parts > 0x7FFFFFFF) return fail(ctx, DIT_ATTN_ERR_LIMIT, "pack has too many work items");
+  const int64_t part_tiles = choose_part_tiles(seqs, few_rows, n_heads, head_dim, ctx->n_cus);
+  p.part_tiles = static_cast<int32_t>(part_tiles);
+  int64_t items = 0, part_rows = 0;
+  for (size_t i = 0; i < order.size(); ++i) {
+    const int64_t parts = parts_of(seqs[i].tiles, part_tiles);
+    items += seqs[i].items * parts;
+    if (parts > 1) part_rows += parts * seqs[i].rows;
+  }
+  if (items > 0x7FFFFFFF) return fail(ctx, DIT_ATTN_ERR_LIMIT, "pack has too many work items");
 
   dit::DeviceGuard guard;
   hipError_t e = guard.enter(ctx->device);
@@ -238,15 +277,15 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
 
   const bool docs = m.q_doc != nullptr;
   const size_t doc_bytes = docs ? (static_cast<size_t>(total_tiles) * sizeof(dit::DocTile) + 255) / 256 * 256 : 0;
-  const size_t part_rh = p.n_parts > 1 ? static_cast<size_t>(p.n_parts) * static_cast<size_t>(total_q) * static_cast<size_t>(n_heads) : 0;
+  const size_t part_rh = static_cast<size_t>(part_rows) * static_cast<size_t>(n_heads);
   const size_t need = doc_bytes + part_rh * (static_cast<size_t>(head_dim) + 1) * sizeof(float);
   if (need > 0) {
     rc = dit::ensure_workspace(ctx, need, dit::stream_capturing(s), "masked attention");
     if (rc != DIT_ATTN_OK) return rc;
     if (docs) p.doc_tiles = reinterpret_cast<dit::DocTile*>(ctx->workspace);
-    if (p.n_parts > 1) {
+    if (part_rows > 0) {
       p.part_out = ctx->workspace + doc_bytes / sizeof(float);
-      p.part_lse = p.part_out + part_rh * head_dim;
+      p.part_lse = p.part_out + part_rh * static_cast<size_t>(head_dim);
     }
   }
   p.q = q;
@@ -254,7 +293,6 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   p.v = v;
   p.out = out;
   p.lse = lse;
-  p.part_rows = total_q;
   p.n_heads = n_heads;
   p.group = group;
   p.c_true = std::fabs(scale) * 1.44269504088896340736f;
@@ -279,24 +317,39 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   p.k_doc = m.k_doc;
   p.slopes = m.slopes;
   p.causal = m.causal;
-  const dit::MaskedKind kind = {head_dim, few_rows, m.softcap > 0.f, m.slopes != nullptr, lse != nullptr || p.n_parts > 1};
+  const dit::MaskedKind kind = {head_dim, few_rows, m.softcap > 0.f, m.slopes != nullptr, lse != nullptr || part_rows > 0};
+  int64_t part_row = 0;
   for (size_t first = 0; first < order.size(); first += dit::kMaskedSeqs) {
     p.n = static_cast<int32_t>(std::min<size_t>(order.size() - first, dit::kMaskedSeqs));
-    uint32_t item = 0, tile = 0;
+    uint32_t item = 0, tile = 0, join = 0;
+    int32_t n_join = 0;  // sequences with several parts come first: they have the most tiles
     for (int32_t i = 0; i < p.n; ++i) {
-      const int32_t sq = order[first + static_cast<size_t>(i)];
+      const size_t at = first + static_cast<size_t>(i);
+      const int32_t sq = order[at];
+      const int64_t parts = parts_of(seqs[at].tiles, part_tiles);
       dit::MaskedSeq& d = p.seq[i];
-      d = {item, tile, cu_q[sq], cu_q[sq + 1] - cu_q[sq], cu_k[sq], cu_k[sq + 1] - cu_k[sq], m.prefix ? m.prefix[sq] : 0};
-      const int64_t blocks = few_rows ? n_kv_heads : (static_cast<int64_t>(d.q_len) + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads;
-      item += static_cast<uint32_t>(blocks * p.n_parts);
-      tile += static_cast<uint32_t>(tiles_of(d.kv_len));
+      d.part_row = part_row;
+      d.first = item;
+      d.tile0 = tile;
+      d.join0 = join;
+      d.q_start = cu_q[sq];
+      d.q_len = cu_q[sq + 1] - cu_q[sq];
+      d.kv_start = cu_k[sq];
+      d.kv_len = cu_k[sq + 1] - cu_k[sq];
+      d.prefix = m.prefix ? m.prefix[sq] : 0;
+      d.parts = static_cast<int32_t>(parts);
+      item += static_cast<uint32_t>(seqs[at].items * parts);
+      tile += static_cast<uint32_t>(seqs[at].tiles);
+      if (parts > 1) {
+        part_row += parts * d.q_len;
+        join += dit::masked_join_blocks(d, n_heads);
+        ++n_join;
+      }
     }
     p.n_items = item;
     e = dit::masked_attn_launch(p, kind, docs ? tile : 0, s);
     if (e != hipSuccess) return fail_hip(ctx, e, "masked attention kernel launch");
-  }
-  if (p.n_parts > 1) {
-    e = dit::masked_join_launch(p, head_dim, s);
+    e = dit::masked_join_launch(p, n_join, join, head_dim, s);
     if (e != hipSuccess) return fail_hip(ctx, e, "join kernel launch");
   }
   return DIT_ATTN_OK;

@@ -23,12 +23,14 @@ namespace dit {
 constexpr float kLn2 = 0.69314718055994530942f;
 [[maybe_unused]] constexpr float kNoReference = -1.0e30f;  // of a row that has seen no key
 
-__device__ __forceinline__ const MaskedSeq& find_seq(const MaskedParams& p, uint32_t idx, bool tiles) {
+// The last of the first n sequences whose FIRST is not behind idx.
+template <uint32_t MaskedSeq::*FIRST>
+__device__ __forceinline__ const MaskedSeq& find_seq(const MaskedParams& p, int n, uint32_t idx) {
   int j = 0;
-  if (p.n > 1) {
+  if (n > 1) {
     static_assert(kMaskedSeqs == 64, "a lane for each sequence");
-    const int lane = threadIdx.x & 63, i = lane < p.n ? lane : 0;
-    j = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < p.n && (tiles ? p.seq[i].tile0 : p.seq[i].first) <= idx));
+    const int lane = threadIdx.x & 63, i = lane < n ? lane : 0;
+    j = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(lane < n && p.seq[i].*FIRST <= idx));
   }
   return p.seq[__builtin_amdgcn_readfirstlane(j)];
 }
@@ -58,7 +60,7 @@ __device__ __forceinline__ DocTile doc_range(const int32_t* ids, int n) {
 __global__ void __launch_bounds__(256) masked_doc_tiles_kernel(MaskedParams p, uint32_t n_tiles) {
   const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (tile >= n_tiles) return;
-  const MaskedSeq& s = find_seq(p, tile, true);
+  const MaskedSeq& s = find_seq<&MaskedSeq::tile0>(p, p.n, tile);
   const int key0 = (int)(tile - s.tile0) * 64;
   const DocTile r = doc_range(p.k_doc + s.kv_start + key0, s.kv_len - key0);
   if ((threadIdx.x & 63) == 0) p.doc_tiles[tile] = r;
@@ -293,15 +295,15 @@ __device__ __forceinline__ void lds_dma_4(const int32_t* base, uint32_t voff, ui
 }
 
 // The rows of a wavefront, O^T / l, leave through LDS as whole rows (see store_out in attn_device.h): bf16 to out, or fp32 halves
-// of rows to the workspace.  inv: 1 / l of the lane's row.
+// of rows to the workspace, from part_row on if that is not negative.  inv: 1 / l of the lane's row.
 template <class T>
-__device__ __forceinline__ void store_rows(const MaskedParams& p, const Lane<T>& L, const ItemU& it, const f32x16 (&o)[T::NDB], float inv,
-                                           uint32_t stage) {
+__device__ __forceinline__ void store_rows(const MaskedParams& p, const Lane<T>& L, const ItemU& it, int64_t part_row,
+                                           const f32x16 (&o)[T::NDB], float inv, uint32_t stage) {
   typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
-  if (p.part_out != nullptr) {
+  if (part_row >= 0) {
     constexpr int CH = T::D / 8, RPS = 64 / CH;  // 16-byte chunks of half a row; half rows per store
     const int ch = L.lane & (CH - 1), r0 = L.lane / CH, row0 = L.wave * 32 + r0, n_valid = it.q_rows - row0;
-    float* const dst = p.part_out + ((((int64_t)it.part * p.part_rows + it.q_start + row0) * p.n_heads) + it.head) * T::D + ch * 4;
+    float* const dst = p.part_out + ((part_row + row0) * p.n_heads + it.head) * T::D + ch * 4;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -479,12 +481,12 @@ masked_attn_kernel(MaskedParams p) {
 
   // The item: heads fastest, so that with a multiple of eight heads an XCD keeps to its own ones; the last query tiles first,
   // which see the most keys under a causal mask.
-  const MaskedSeq& sq = find_seq(p, blockIdx.x, false);
+  const MaskedSeq& sq = find_seq<&MaskedSeq::first>(p, p.n, blockIdx.x);
   const int n_heads = p.n_heads, lq = sq.q_len, lk = sq.kv_len;
   uint32_t local = blockIdx.x - sq.first;
   ItemU it;
-  it.part = (int)(local % (uint32_t)p.n_parts);
-  local /= (uint32_t)p.n_parts;
+  it.part = (int)(local % (uint32_t)sq.parts);
+  local /= (uint32_t)sq.parts;
   it.head = (int)(local % (uint32_t)n_heads);
   const int m0 = ((lq + T::BM - 1) / T::BM - 1 - (int)(local / (uint32_t)n_heads)) * T::BM;
   it.q_start = sq.q_start + m0;
@@ -803,13 +805,14 @@ masked_attn_kernel(MaskedParams p) {
 
   const float l = r.l + __shfl_xor(r.l, 32), lx = r.lx + __shfl_xor(r.lx, 32);
   const bool any = l > 0.f || l != l;
-  store_rows<T>(p, fresh_lane(), it, o, any ? 1.f / l : 0.f, lds + T::K_OFF + (uint32_t)wave * (32 * T::ROW_B));
+  const int64_t part_row = sq.parts > 1 ? sq.part_row + (int64_t)it.part * lq + m0 : -1;
+  store_rows<T>(p, fresh_lane(), it, part_row, o, any ? 1.f / l : 0.f, lds + T::K_OFF + (uint32_t)wave * (32 * T::ROW_B));
   if constexpr (LSE) {
     const int qrow = wave * 32 + (tid & 31);
     if (qrow < it.q_rows && (tid & 32) == 0) {
       const float c = CAP || BIAS ? 1.f : p.c_log2;
-      float* dst = p.part_out != nullptr ? p.part_lse + (int64_t)it.part * p.part_rows * n_heads : p.lse;
-      dst[(int64_t)(it.q_start + qrow) * n_heads + it.head] = any ? kLn2 * (r.m_ref * c + __builtin_amdgcn_logf(lx)) : -__builtin_inff();
+      float* dst = part_row >= 0 ? p.part_lse + (part_row + qrow) * n_heads : p.lse + (int64_t)(it.q_start + qrow) * n_heads;
+      if (part_row >= 0 || p.lse != nullptr) dst[it.head] = any ? kLn2 * (r.m_ref * c + __builtin_amdgcn_logf(lx)) : -__builtin_inff();
     }
   }
 #endif
@@ -817,24 +820,28 @@ masked_attn_kernel(MaskedParams p) {
 
 // ---------------------------------------------------------------------------------------------
 // Few query rows (one new token, say): every (row, query head of a key head's group) is a column, at most 32 of them, so that
-// K and V are read once for the whole group.  Bound by reading them.  The four wavefronts take 32-key blocks in turn, each
-// with loads, LDS and softmax state of its own and no barrier until the end, when their four results are joined.
+// K and V are read once for the whole group.  Bound by reading them.  Eight wavefronts take blocks of keys in turn, each with
+// loads, LDS and softmax state of its own and no barrier until the end, when their results are joined.  A wavefront's K buffer
+// takes the next block as soon as the scores are contracted, its V buffer as soon as O^T is: two wavefronts on a SIMD keep both
+// in flight, 128 KB a compute unit.
 // ---------------------------------------------------------------------------------------------
 template <int D>
 struct FewRows {
-  using T = Tile<D, 4, 32>;
-  static constexpr int STAGES = D == 128 ? 2 : 4;
-  static constexpr int BLOCK_B = 32 * T::ROW_B;          // 32 keys of K or V
-  static constexpr int WAVE_B = STAGES * 2 * BLOCK_B;    // [stage][K, V]
-  static constexpr int DOCS_OFF = 4 * WAVE_B;            // [wave][stage][32] ids
-  static constexpr int STATE_OFF = DOCS_OFF + 4 * STAGES * 128;  // [m, l, lx][wave][column]
-  static constexpr int LDS_BYTES = STATE_OFF + 3 * 4 * 32 * 4;
-  static constexpr int N = 32 / T::RPI;                  // load instructions of a block of K or V
-  static_assert(32 * D * 4 <= WAVE_B, "a wavefront's result fits its stages");
+  static constexpr int KEYS = 4096 / D;                    // of a block: 8 KB of K and of V
+  using T = Tile<D, 4, KEYS>;
+  static constexpr int WAVES = 8;
+  static constexpr int BLOCK_B = KEYS * T::ROW_B;
+  static constexpr int WAVE_B = 2 * BLOCK_B;               // [K, V]
+  static constexpr int DOCS_OFF = WAVES * WAVE_B;          // [wave][2][KEYS] ids
+  static constexpr int DOCS_B = KEYS * 4;
+  static constexpr int STATE_OFF = DOCS_OFF + WAVES * 2 * DOCS_B;  // [m, l, lx][wave][column]
+  static constexpr int LDS_BYTES = STATE_OFF + 3 * WAVES * 32 * 4;
+  static constexpr int N = KEYS / T::RPI;                  // load instructions of a block of K or V
+  static_assert(32 * D * 4 <= WAVE_B, "a wavefront's result fits its buffers");
 };
 
 template <int D, bool CAP, bool BIAS>
-__global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(1, 1))) masked_few_rows_kernel(MaskedParams p) {
+__global__ void __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_waves_per_eu(2, 2))) masked_few_rows_kernel(MaskedParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using F = FewRows<D>;
   using T = typename F::T;
@@ -846,12 +853,19 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
   L.init(tid, p.k_stride_b);
   const int wave = L.wave, hh = L.hh;
 
-  const MaskedSeq& sq = find_seq(p, blockIdx.x, false);
+  const MaskedSeq& sq = find_seq<&MaskedSeq::first>(p, p.n, blockIdx.x);
   const int lq = sq.q_len, lk = sq.kv_len, group = p.group, n_heads = p.n_heads;
   uint32_t local = blockIdx.x - sq.first;
-  const int part = (int)(local % (uint32_t)p.n_parts), kv_head = (int)(local / (uint32_t)p.n_parts);
+  const int part = (int)(local % (uint32_t)sq.parts), kv_head = (int)(local / (uint32_t)sq.parts);
   const int n_cols = lq * group;
-  const int col = L.l32 < n_cols ? L.l32 : n_cols - 1, row = col / group, head = kv_head * group + (col - row * group);
+  // This lane's column, or the last one, as its row and head.
+  auto column = [&](int& head) {
+    int x = tid;
+    asm volatile("" : "+v"(x));
+    const int c = (x & 31) < n_cols ? (x & 31) : n_cols - 1, row = c / group;
+    head = kv_head * group + (c - row * group);
+    return row;
+  };
 
   const int pos0 = lk - lq;
   auto row_limit = [&](int i) {
@@ -860,7 +874,6 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
     return k < lk ? k : lk;
   };
   const int lim = row_limit(lq - 1), klim_first = row_limit(0);
-  int klim = row_limit(row);
 
   LiveTiles tiles;
   tiles.ranges = nullptr;
@@ -872,26 +885,31 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
   if ((int64_t)part * p.part_tiles < nt) t0 = part * p.part_tiles;
   tiles.end = part_end < nt ? (int)part_end : nt;
   const bool have_docs = p.q_doc != nullptr;
-  int doc = 0;
   const int32_t* kdoc = nullptr;
   if (have_docs) {
     kdoc = p.k_doc + sq.kv_start;
-    doc = p.q_doc[sq.q_start + row];
-    if (doc < 0) klim = 0;  // sees nothing
     tiles.mine = doc_range(p.q_doc + sq.q_start, lq);
     tiles.ranges = p.doc_tiles + sq.tile0;
   }
-  // Blocks of 32 keys; this wavefront's are wave, wave + 4, ... of those in live tiles.
-  const int n_blocks = tiles.end * 2 < (lim + 31) / 32 ? tiles.end * 2 : (lim + 31) / 32;
+  // The id of this lane's row, and the keys that the row sees are under the limit.
+  auto row_mask = [&](int& doc) {
+    int head;
+    const int row = column(head);
+    doc = have_docs ? p.q_doc[sq.q_start + row] : 0;
+    return doc < 0 ? 0 : row_limit(row);
+  };
+  // Blocks of keys; this wavefront's are wave, wave + 8, ... of those in live tiles.
+  constexpr int BPT = 64 / F::KEYS;  // blocks of a tile
+  const int all_blocks = (lim + F::KEYS - 1) / F::KEYS, n_blocks = tiles.end * BPT < all_blocks ? tiles.end * BPT : all_blocks;
   auto next_block = [&](int b) {
     while (b < n_blocks) {
-      const int t = tiles.next(b >> 1);
-      if (t == b >> 1) return b;
-      b += (2 * t - b + 3) & ~3;
+      const int t = tiles.next(b / BPT);
+      if (t == b / BPT) return b;
+      b += (BPT * t - b + F::WAVES - 1) & ~(F::WAVES - 1);
     }
     return n_blocks;
   };
-  const int first_block = t0 * 2 + ((wave - t0 * 2) & 3);
+  const int first_block = t0 * BPT + ((wave - t0 * BPT) & (F::WAVES - 1));
 
   f32x16 o[T::NDB];
 #pragma unroll
@@ -900,34 +918,54 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   RowState r = {kNoReference, 0.f, 0.f};
   const float c = CAP || BIAS ? 1.f : p.c_log2;
-  const uint32_t ring = lds + (uint32_t)wave * F::WAVE_B, docs = lds + F::DOCS_OFF + (uint32_t)wave * (F::STAGES * 128);
+  const uint32_t kbuf = lds + (uint32_t)wave * F::WAVE_B, vbuf = kbuf + F::BLOCK_B, docs = lds + F::DOCS_OFF + (uint32_t)wave * (2 * F::DOCS_B);
 
   int block = t0 < tiles.end ? next_block(first_block) : n_blocks;
   if (block < n_blocks) {
     const char* kbase = static_cast<const char*>(p.k) + (int64_t)sq.kv_start * p.k_stride_b + (int64_t)kv_head * T::ROW_B;
     const char* vbase = static_cast<const char*>(p.v) + (int64_t)sq.kv_start * p.v_stride_b + (int64_t)kv_head * T::ROW_B;
+    int head;
+    const int row = column(head);
     const float slope = BIAS ? p.slopes[head] * 1.44269504088896340736f : 0.f;
-    const int at = L.lane % T::CPR, q = L.lane / T::CPR;  // chunk and row of this lane in one load instruction
-    const uint32_t vcol = (uint32_t)((at ^ T::swz_v(q)) * 16);
-
-    auto load = [&](int b, int stage) {
-      const int key0 = b * 32, last = lim - 1 - key0;
-      const uint32_t dst = ring + (uint32_t)stage * (2 * F::BLOCK_B);
-      const char* kb = kbase + (int64_t)key0 * p.k_stride_b;
-      const char* vb = vbase + (int64_t)key0 * p.v_stride_b;
+    const int at0 = BIAS ? pos0 + row - 4 * hh : 0;
+    // Lane offsets of the load instructions, RPI rows each: a V row's chunk order has a period of one, a K row's of KN.
+    constexpr int KN = 16 / T::RPI;
+    uint32_t koff[KN], voff;
+    {
+      const int at = L.lane % T::CPR, q = L.lane / T::CPR;  // chunk and row
 #pragma unroll
-      for (int i = 0; i < F::N; ++i) {
-        int rr = i * T::RPI + q;
-        const uint32_t kcol = (uint32_t)((at ^ T::swz_k(rr)) * 16);
-        rr = rr < last ? rr : last;
-        lds_dma_16(kb, (uint32_t)rr * (uint32_t)p.k_stride_b + kcol, dst + i * 1024);
-        lds_dma_16(vb, (uint32_t)rr * (uint32_t)p.v_stride_b + vcol, dst + F::BLOCK_B + i * 1024);
-      }
-      if (have_docs) {
-        const int k = L.l32 < last ? L.l32 : last;
-        if (L.hh == 0) lds_dma_4(kdoc + key0, (uint32_t)k * 4u, docs + (uint32_t)stage * 128u);
+      for (int i = 0; i < KN; ++i) koff[i] = (uint32_t)q * (uint32_t)p.k_stride_b + (uint32_t)((at ^ T::swz_k(i * T::RPI + q)) * 16);
+      voff = (uint32_t)q * (uint32_t)p.v_stride_b + (uint32_t)((at ^ T::swz_v(q)) * 16);
+      static_assert(T::swz_k(16) == T::swz_k(0) && T::swz_v(T::RPI) == T::swz_v(0), "periods");
+    }
+    auto load_rows = [&](auto is_k, const char* base, int64_t stride_b, int key0, uint32_t buf) {
+      constexpr bool K = decltype(is_k)::value != 0;
+      const char* b = base + (int64_t)key0 * stride_b;
+      if (key0 + F::KEYS <= lim) {
+#pragma unroll
+        for (int i = 0; i < F::N; ++i) lds_dma_16(b + (int64_t)(i * T::RPI) * stride_b, K ? koff[i % KN] : voff, buf + i * 1024);
+      } else {  // rows past the last key re-read it (they are dead)
+        int lane = tid & 63;
+        asm volatile("" : "+v"(lane));
+        const int at = lane % T::CPR, q = lane / T::CPR, last = lim - 1 - key0;
+#pragma unroll
+        for (int i = 0; i < F::N; ++i) {
+          const int rr = i * T::RPI + q, from = rr < last ? rr : last;
+          lds_dma_16(b, (uint32_t)from * (uint32_t)stride_b + (uint32_t)((at ^ (K ? T::swz_k(rr) : T::swz_v(rr))) * 16), buf + i * 1024);
+        }
       }
     };
+    int turn = 0;  // of the ids
+    auto load_k = [&](int b, int to) {
+      const int key0 = b * F::KEYS;
+      load_rows(IC<1>{}, kbase, p.k_stride_b, key0, kbuf);
+      if (have_docs) {
+        const int last = lim - 1 - key0, k = L.lane < last ? L.lane : last;
+        if (L.lane < F::KEYS) lds_dma_4(kdoc + key0, (uint32_t)k * 4u, docs + (uint32_t)(to * F::DOCS_B));
+      }
+    };
+    load_k(block, 0);
+    load_rows(IC<0>{}, vbase, p.v_stride_b, block * F::KEYS, vbuf);
 
     bf16x8 qf[T::NKS];
     {
@@ -940,32 +978,35 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
       }
     }
     int ka[T::NKS], va[T::NDB];
+    L.operand_addrs(kbuf - T::K_OFF, vbuf - T::V_OFF, ka, va);
     bool poison = false;
-    // The blocks in flight, oldest first, and whether every row sees all of their keys' documents; n_blocks stands for none.
-    int queue[F::STAGES];
-    bool pure[F::STAGES];
-    auto take = [&](int i, int b, int to_stage) {
-      queue[i] = b;
-      pure[i] = b < n_blocks && tiles.is_pure(b >> 1);
-      if (b < n_blocks) load(b, to_stage);
-    };
-    take(0, block, 0);
-#pragma unroll
-    for (int i = 1; i < F::STAGES; ++i) take(i, queue[i - 1] < n_blocks ? next_block(queue[i - 1] + 4) : n_blocks, i);
-    int stage = 0;
-    while (queue[0] < n_blocks) {
-      // The oldest block has landed when at most the later ones' loads are outstanding.
-      if (queue[F::STAGES - 1] < n_blocks) {
-        if (have_docs) wait_loads_but<(F::STAGES - 1) * (2 * F::N + 1)>();
-        else wait_loads_but<(F::STAGES - 1) * 2 * F::N>();
-      } else {
-        wait_loads();
-      }
-      const int key0 = queue[0] * 32;
-      const uint32_t kbuf = ring + (uint32_t)stage * (2 * F::BLOCK_B), vbuf = kbuf + F::BLOCK_B;
-      const bool masked = klim_first < key0 + 32 || !pure[0];
-      uint32_t bad = 0;
+    while (block < n_blocks) {
+      const int key0 = block * F::KEYS;
+      const bool masked = klim_first < key0 + F::KEYS || !tiles.is_pure(block / BPT);
+      const int next = next_block(block + F::WAVES);
+      wait_loads_but<F::N>();  // V may be outstanding
+      f32x16 s[T::NKB];
+      uint32_t pb[T::NKB][8];
+      mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, s);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
+      if (next < n_blocks) load_k(next, turn ^ 1);
+      if constexpr (CAP || BIAS) shape_scores<T::NKB, CAP, BIAS>(s, p, false, slope, at0 - key0);
       if (masked) {
+        int doc;
+        const int n = row_mask(doc) - key0;
+        const LaneMask m = {-4 * hh, n > 0 ? (unsigned)n : 0u};
+        mask_scores<T::NKB>(s, m, have_docs, docs + (uint32_t)(turn * F::DOCS_B), doc, hh);
+      }
+#pragma unroll
+      for (int kb = 0; kb < T::NKB; ++kb) asm volatile("s_nop 11" : "+v"(s[kb]));  // as scores_ready
+      const float mx = tile_max<T>(s);
+      masked_softmax<T::NKB, T::NDB, true>(s, mx, c, pb, o, r);
+      // V has landed when only the next K (and its ids) may be outstanding.
+      if (next >= n_blocks) wait_loads();
+      else if (have_docs) wait_loads_but<F::N + 1>();
+      else wait_loads_but<F::N>();
+      if (masked) {
+        uint64_t bad = 0;
         const uint32_t found = make_finite<F::N>(vbuf + (uint32_t)L.lane * 16u, 1024);
         if (__builtin_amdgcn_ballot_w64(found != 0) != 0) {
 #pragma unroll
@@ -973,42 +1014,27 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
             const uint64_t rows = __builtin_amdgcn_ballot_w64((found >> i & 1) != 0);
 #pragma unroll
             for (int k = 0; k < T::RPI; ++k)
-              if ((rows >> (k * T::CPR)) & ((1ull << T::CPR) - 1)) bad |= 1u << (i * T::RPI + k);
+              if ((rows >> (k * T::CPR)) & ((1ull << T::CPR) - 1)) bad |= 1ull << (i * T::RPI + k);
           }
+          poison |= sees<T::NKB>(s, bad, hh);
         }
         asm volatile("" ::: "memory");
       }
-      L.operand_addrs(kbuf - T::K_OFF, vbuf - T::V_OFF, ka, va);
-      f32x16 s[1];
-      uint32_t pb[1][8];
-      mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, s);
-      if constexpr (CAP || BIAS) shape_scores<1, CAP, BIAS>(s, p, false, slope, pos0 + row - key0 - 4 * hh);
-      if (masked) {
-        const int n = klim - key0;
-        const LaneMask m = {-4 * hh, n > 0 ? (unsigned)n : 0u};
-        mask_scores<1>(s, m, have_docs, docs + (uint32_t)stage * 128u, doc, hh);
-        if (bad != 0) poison |= sees<1>(s, bad, hh);
-      }
-      asm volatile("s_nop 11" : "+v"(s[0]));  // as scores_ready
-      const float mx = tile_max<T>(s);
-      masked_softmax<1, T::NDB, true>(s, mx, c, pb, o, r);
       mfma_stream<T, true, 0, 0, kPrefetch>(smem, va, ka, pb, qf, o, s);
       r.l += row_sum<T>(pb);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this stage has been read
-      const int youngest = queue[F::STAGES - 1];
-#pragma unroll
-      for (int i = 0; i + 1 < F::STAGES; ++i) {
-        queue[i] = queue[i + 1];
-        pure[i] = pure[i + 1];
-      }
-      take(F::STAGES - 1, youngest < n_blocks ? next_block(youngest + 4) : n_blocks, stage);
-      stage = stage == F::STAGES - 1 ? 0 : stage + 1;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
+      if (next < n_blocks) load_rows(IC<0>{}, vbase, p.v_stride_b, next * F::KEYS, vbuf);
+      block = next;
+      turn ^= 1;
     }
-    if (__builtin_amdgcn_ballot_w64(poison) != 0)
-      add_not_finite<T>(p, vbase, kdoc, first_block * 32, n_blocks * 32 < lim ? n_blocks * 32 : lim, 32, 128, klim, doc, hh, o);
+    if (__builtin_amdgcn_ballot_w64(poison) != 0) {
+      int doc;
+      const int klim = row_mask(doc);
+      add_not_finite<T>(p, vbase, kdoc, first_block * F::KEYS, n_blocks * F::KEYS < lim ? n_blocks * F::KEYS : lim, F::KEYS, F::KEYS * F::WAVES, klim, doc, hh, o);
+    }
   }
 
-  // The four results, unnormalised, through the wavefronts' own stages: 16-byte chunk j of column i at j ^ i.
+  // The results, unnormalised, through the wavefronts' own buffers: 16-byte chunk j of column i at j ^ i.
   constexpr int CH = D / 4;
 #pragma unroll
   for (int db = 0; db < T::NDB; ++db)
@@ -1016,43 +1042,43 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
     for (int g = 0; g < 4; ++g) {
       const int ch = 8 * db + 2 * g + hh;
       const f32x4 f = {o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
-      *(lds_u32x4*)(uintptr_t)(ring + (uint32_t)(L.l32 * (D * 4) + ((ch ^ (L.l32 & (CH - 1))) * 16))) = __builtin_bit_cast(u32x4, f);
+      *(lds_u32x4*)(uintptr_t)(kbuf + (uint32_t)(L.l32 * (D * 4) + ((ch ^ (L.l32 & (CH - 1))) * 16))) = __builtin_bit_cast(u32x4, f);
     }
   typedef __attribute__((address_space(3))) float lds_f32;
   const uint32_t state = lds + F::STATE_OFF;
   const float l = r.l + __shfl_xor(r.l, 32), lx = r.lx + __shfl_xor(r.lx, 32);
   if (hh == 0) {
     *(lds_f32*)(uintptr_t)(state + (uint32_t)(wave * 32 + L.l32) * 4u) = l > 0.f || l != l ? r.m_ref * c : -__builtin_inff();
-    *(lds_f32*)(uintptr_t)(state + (uint32_t)(128 + wave * 32 + L.l32) * 4u) = l;
-    *(lds_f32*)(uintptr_t)(state + (uint32_t)(256 + wave * 32 + L.l32) * 4u) = lx;
+    *(lds_f32*)(uintptr_t)(state + (uint32_t)(F::WAVES * 32 + wave * 32 + L.l32) * 4u) = l;
+    *(lds_f32*)(uintptr_t)(state + (uint32_t)(2 * F::WAVES * 32 + wave * 32 + L.l32) * 4u) = lx;
   }
   wg_barrier();
-  for (int e = tid; e < n_cols * CH; e += 256) {
+  for (int e = tid; e < n_cols * CH; e += 64 * F::WAVES) {
     const int cc = e / CH, ch = e % CH;
-    float m[4], w[4], top = -__builtin_inff(), sum = 0.f, sumx = 0.f;
+    float m[F::WAVES], top = -__builtin_inff(), sum = 0.f, sumx = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < F::WAVES; ++i) {
       m[i] = *(lds_f32*)(uintptr_t)(state + (uint32_t)(i * 32 + cc) * 4u);
       top = __builtin_fmaxf(top, m[i]);
     }
     if (top == -__builtin_inff()) top = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = __builtin_amdgcn_exp2f(m[i] - top);
-      sum = __builtin_fmaf(w[i], *(lds_f32*)(uintptr_t)(state + (uint32_t)(128 + i * 32 + cc) * 4u), sum);
-      sumx = __builtin_fmaf(w[i], *(lds_f32*)(uintptr_t)(state + (uint32_t)(256 + i * 32 + cc) * 4u), sumx);
+    for (int i = 0; i < F::WAVES; ++i) {
+      const float w = __builtin_amdgcn_exp2f(m[i] - top);
+      sum = __builtin_fmaf(w, *(lds_f32*)(uintptr_t)(state + (uint32_t)((F::WAVES + i) * 32 + cc) * 4u), sum);
+      sumx = __builtin_fmaf(w, *(lds_f32*)(uintptr_t)(state + (uint32_t)((2 * F::WAVES + i) * 32 + cc) * 4u), sumx);
       const f32x4 f = __builtin_bit_cast(f32x4, *(lds_u32x4*)(uintptr_t)(lds + (uint32_t)(i * F::WAVE_B + cc * (D * 4) + ((ch ^ (cc & (CH - 1))) * 16))));
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc[k] = __builtin_fmaf(w[i], f[k], acc[k]);
+      for (int k = 0; k < 4; ++k) acc[k] = __builtin_fmaf(w, f[k], acc[k]);
     }
     const bool any = sum > 0.f || sum != sum;
     const float inv = any ? 1.f / sum : 0.f;
     const int rr = cc / group, hd = kv_head * group + (cc - rr * group);
     const int64_t rh = (int64_t)(sq.q_start + rr) * n_heads + hd;
     const float row_lse = any ? kLn2 * (top + __builtin_amdgcn_logf(sumx)) : -__builtin_inff();
-    if (p.part_out != nullptr) {
-      const int64_t prh = (int64_t)part * p.part_rows * n_heads + rh;
+    if (sq.parts > 1) {
+      const int64_t prh = (sq.part_row + (int64_t)part * lq + rr) * n_heads + hd;
       const f32x4 y = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
       store_through(reinterpret_cast<u32x4*>(p.part_out + prh * D + ch * 4), __builtin_bit_cast(u32x4, y));
       if (ch == 0) p.part_lse[prh] = row_lse;
@@ -1066,36 +1092,55 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_wav
 }
 
 // ---------------------------------------------------------------------------------------------
-// out = sum over parts exp(lse_part - lse) O_part,  eight elements a thread.  Bound by the parts, which lie in the memory-side cache.
+// out = sum over parts exp(lse_part - lse) O_part.  A wavefront for a (row, head): a lane holds the weight of a part, then two
+// elements (D 64: one) of the row.  Two latencies, of the parts' lse and of the parts themselves.
 // ---------------------------------------------------------------------------------------------
+constexpr int kJoinRows = 4;  // (row, head)s of a workgroup
+
 template <int D>
-__global__ void __launch_bounds__(256) masked_join_kernel(const float* part_out, const float* part_lse, void* out, float* lse, int64_t n_rh,
-                                                          int n_parts) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, rh = e / (D / 8);
+__global__ void __launch_bounds__(256) masked_join_kernel(MaskedParams p, int32_t n) {
+  typedef __attribute__((__vector_size__(D / 64 * sizeof(float)))) float elems;
+  const MaskedSeq& sq = find_seq<&MaskedSeq::join0>(p, n, blockIdx.x);
+  const int lane = threadIdx.x & 63, parts = sq.parts;
+  const int64_t rh = (int64_t)(blockIdx.x - sq.join0) * kJoinRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n_rh = (int64_t)sq.q_len * p.n_heads;
   if (rh >= n_rh) return;
-  float top = -__builtin_inff();
-  for (int i = 0; i < n_parts; ++i) top = __builtin_fmaxf(top, part_lse[i * n_rh + rh]);
+  const int64_t rh0 = sq.part_row * p.n_heads + rh;
+  static_assert(kMaskedMaxParts == 64, "a lane for each part");
+  const float part_lse = lane < parts ? p.part_lse[rh0 + lane * n_rh] : -__builtin_inff();
+  const float* src = p.part_out + rh0 * D + lane * (D / 64);
+  float top = part_lse;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, d));
   if (top == -__builtin_inff()) top = 0.f;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-  for (int i = 0; i < n_parts; ++i) {
-    const float w = __builtin_amdgcn_exp2f((part_lse[i * n_rh + rh] - top) * 1.44269504088896340736f);
-    const f32x4* src = reinterpret_cast<const f32x4*>(part_out + (i * n_rh * D + e * 8));
-    const f32x4 a = src[0], b = src[1];
-    sum += w;
-    if (w != 0.f)  // a part without keys has left its values unwritten or zero
+  const float w = __builtin_amdgcn_exp2f((part_lse - top) * 1.44269504088896340736f);
+  float sum = w;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        acc[k] = __builtin_fmaf(w, a[k], acc[k]);
-        acc[4 + k] = __builtin_fmaf(w, b[k], acc[4 + k]);
-      }
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  elems acc = {};
+  auto add = [&](elems x, int i) {
+    const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i));
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) acc[k] = __builtin_fmaf(wi, wi != 0.f ? x[k] : 0.f, acc[k]);  // unseen: no weight, unwritten
+  };
+  int i = 0;
+  for (; i + 8 <= parts; i += 8) {
+    elems x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const elems*>(src + (i + j) * n_rh * D);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) add(x[j], i + j);
   }
-  const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-  u32x4 y;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) y[k] = pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
-  store_through(reinterpret_cast<u32x4*>(out) + e, y);
-  if (lse != nullptr && (e & (D / 8 - 1)) == 0)
-    lse[rh] = sum > 0.f || sum != sum ? top + kLn2 * __builtin_amdgcn_logf(sum) : -__builtin_inff();
+  for (; i < parts; ++i) add(*reinterpret_cast<const elems*>(src + i * n_rh * D), i);
+  const bool any = sum > 0.f || sum != sum;
+  const float inv = any ? 1.f / sum : 0.f;
+  const int64_t to = (int64_t)sq.q_start * p.n_heads + rh;
+  if constexpr (D == 128) {
+    static_cast<uint32_t*>(p.out)[to * 64 + lane] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  } else {
+    static_cast<__bf16*>(p.out)[to * 64 + lane] = (__bf16)(acc[0] * inv);
+  }
+  if (p.lse != nullptr && lane == 0) p.lse[to] = any ? top + kLn2 * __builtin_amdgcn_logf(sum) : -__builtin_inff();
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1104,15 +1149,15 @@ __global__ void __launch_bounds__(256) masked_join_kernel(const float* part_out,
 using MaskedKernel = void (*)(MaskedParams);
 struct MaskedEntry {
   MaskedKernel fn;
-  int lds;
+  int lds, threads;
 };
 
 template <int D, bool CAP, bool BIAS>
 static MaskedEntry entry_of(bool few_rows, bool lse) {
   using T = Tile<D, 4, 64>;
-  if (few_rows) return {masked_few_rows_kernel<D, CAP, BIAS>, FewRows<D>::LDS_BYTES};
-  if (lse) return {masked_attn_kernel<T, CAP, BIAS, true>, kMaskedLds<T>};
-  return {masked_attn_kernel<T, CAP, BIAS, false>, kMaskedLds<T>};
+  if (few_rows) return {masked_few_rows_kernel<D, CAP, BIAS>, FewRows<D>::LDS_BYTES, 64 * FewRows<D>::WAVES};
+  if (lse) return {masked_attn_kernel<T, CAP, BIAS, true>, kMaskedLds<T>, T::NT};
+  return {masked_attn_kernel<T, CAP, BIAS, false>, kMaskedLds<T>, T::NT};
 }
 template <int D>
 static MaskedEntry entry_of(const MaskedKind& k) {
@@ -1139,15 +1184,18 @@ hipError_t masked_attn_launch(const MaskedParams& p, const MaskedKind& kind, uin
     if (e != hipSuccess) return e;
   }
   const MaskedEntry m = entry_of(kind);
-  hipLaunchKernelGGL(m.fn, dim3(p.n_items), dim3(256), m.lds, stream, p);
+  hipLaunchKernelGGL(m.fn, dim3(p.n_items), dim3(m.threads), m.lds, stream, p);
   return hipGetLastError();
 }
 
-hipError_t masked_join_launch(const MaskedParams& p, int head_dim, hipStream_t stream) {
-  const int64_t n_rh = p.part_rows * p.n_heads, blocks = (n_rh * (head_dim / 8) + 255) / 256;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+uint32_t masked_join_blocks(const MaskedSeq& s, int n_heads) {
+  return (uint32_t)(((int64_t)s.q_len * n_heads + kJoinRows - 1) / kJoinRows);
+}
+
+hipError_t masked_join_launch(const MaskedParams& p, int32_t n, uint32_t n_blocks, int head_dim, hipStream_t stream) {
+  if (n == 0) return hipSuccess;
   const auto fn = head_dim == 64 ? masked_join_kernel<64> : masked_join_kernel<128>;
-  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(256), 0, stream, p.part_out, p.part_lse, p.out, p.lse, n_rh, p.n_parts);
+  hipLaunchKernelGGL(fn, dim3(n_blocks), dim3(256), 0, stream, p, n);
   return hipGetLastError();
 }
 

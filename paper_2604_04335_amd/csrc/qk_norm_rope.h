@@ -13,8 +13,8 @@ struct RopeTableParams {
   int64_t n_rows;
   int32_t n_axes, n_pairs;
   float magnitude;
-  // Turns per position of every pair, as the sum of two doubles, and the axis of its position.
-  double turns_hi[kMaxRopePairs], turns_lo[kMaxRopePairs];
+  // Quarter turns per position of every pair, as the sum of two doubles, and the axis of its position.
+  double quarters_hi[kMaxRopePairs], quarters_lo[kMaxRopePairs];
   uint8_t axis[kMaxRopePairs];
 };
 hipError_t rope_table_launch(const RopeTableParams& p, hipStream_t stream);

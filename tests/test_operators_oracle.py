@@ -103,9 +103,10 @@ def test_binding_structures():
     import torch
     t = torch.zeros((5, 12 * 64), dtype=torch.bfloat16)
     side = da.NormHeads(t[:, :256].unflatten(1, (4, 64)), torch.zeros((5, 4, 64), dtype=torch.bfloat16))
-    assert side.row_stride == 768 and side.out_row_stride == 256 and side.n_heads == 4
+    assert side.row_stride == 768 and side.out_row_stride == 0 and side.n_heads == 4
     one = torch.zeros((1, 4, 64), dtype=torch.bfloat16)
-    assert da.NormHeads(one, one).row_stride == 256
+    assert da.NormHeads(one, one).row_stride == 0
+    assert da.NormHeads(t[:1, :256].unflatten(1, (4, 64)), one).row_stride == 0
     for bad in (torch.zeros((5, 4, 64)), torch.zeros((5, 64, 4), dtype=torch.bfloat16).transpose(1, 2),
                 torch.zeros((4, 5, 64), dtype=torch.bfloat16).transpose(0, 1)):
         with pytest.raises(ValueError):
