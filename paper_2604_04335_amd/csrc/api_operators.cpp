@@ -295,17 +295,17 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   p.lse = lse;
   p.n_heads = n_heads;
   p.group = group;
-  p.c_true = std::fabs(scale) * 1.44269504088896340736f;
-  p.c_log2 = std::max(p.c_true, 1e-30f);
+  // Never 0, so that a dead score of -inf times it stays -inf; with a bias, whose slopes are divided by it, further from 0.
+  p.c_log2 = std::max(std::fabs(scale) * 1.44269504088896340736f, m.slopes ? 1e-20f : 1e-30f);
   p.negate = scale < 0.f ? 1 : 0;
   if (m.softcap > 0.f) {
     p.tanh_in = static_cast<float>(2.0 * 1.44269504088896340736 * std::fabs(static_cast<double>(scale)) / m.softcap);
     p.cap_log2 = m.softcap * 1.44269504088896340736f;
-    // tanh(x) / x as a polynomial in x^2, off by at most 1e-7 relative for |x| <= 0.4 (a fit of least maximal error).
-    const double a[4] = {0.9999999019008419, -0.3333136245791241, 0.13270976741775176, -0.04755360290962831};
+    // tanh(x) / x as a polynomial in x^2, off by at most 4e-7 relative for |x| <= 0.25 (a fit of least maximal error).
+    const double a[3] = {0.9999996043443452, -0.33321908223103114, 0.12841613400294474};
     const double k = std::fabs(static_cast<double>(scale)) / m.softcap;
-    p.small = static_cast<float>(0.4 / k);  // scale 0: infinite
-    for (int i = 0; i < 4; ++i) {
+    p.small = static_cast<float>(0.25 / k);  // scale 0: infinite
+    for (int i = 0; i < 3; ++i) {
       p.poly[i] = static_cast<float>(a[i] * m.softcap * 1.44269504088896340736 * std::pow(k, 2 * i + 1));
       if (!std::isfinite(p.poly[i])) p.small = -1.f;  // never
     }

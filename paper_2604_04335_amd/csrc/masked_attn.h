@@ -34,10 +34,9 @@ struct MaskedParams : AttnParams {
   const int32_t* k_doc;    // [Tk]
   DocTile* doc_tiles;
   const float* slopes;     // [n_heads] or nullptr
-  float c_true;            // |scale| * log2(e)
   float tanh_in;           // 2 * log2(e) * |scale| / cap
   float cap_log2;          // cap * log2(e)
-  float small, poly[4];    // cap: raw scores up to `small` take s (poly[0] + poly[1] s^2 + poly[2] s^4 + poly[3] s^6)
+  float small, poly[3];    // cap: raw scores up to `small` take s (poly[0] + poly[1] s^2 + poly[2] s^4)
   int32_t causal;
   int32_t group;           // query heads per key head
   int32_t part_tiles;      // 64-key tiles of a part

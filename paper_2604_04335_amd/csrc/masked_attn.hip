@@ -21,7 +21,7 @@
 namespace dit {
 
 constexpr float kLn2 = 0.69314718055994530942f;
-[[maybe_unused]] constexpr float kNoReference = -1.0e30f;  // of a row that has seen no key
+[[maybe_unused]] constexpr float kNoReference = -3.0e38f;  // of a row that has seen no key
 
 // The last of the first n sequences whose FIRST is not behind idx.
 template <uint32_t MaskedSeq::*FIRST>
@@ -48,12 +48,13 @@ __device__ __forceinline__ int wave_max(int x) { return ~wave_min(~x); }
 // Ids of n consecutive places from ids, one a lane (n at most 64 counts).
 __device__ __forceinline__ DocTile doc_range(const int32_t* ids, int n) {
   const int lane = threadIdx.x & 63;
-  const int id = ids[lane < n ? lane : 0];
-  DocTile r;
-  r.any_lo = wave_min(id);
-  r.lo = wave_min(id < 0 ? INT32_MAX : id);
-  r.hi = wave_max(id < 0 ? -1 : id);
-  r.unused = 0;
+  const int id = ids[lane < n ? lane : 0], one = __builtin_amdgcn_readfirstlane(id);
+  DocTile r = {one, one, one, 0};
+  if (one < 0 || __builtin_amdgcn_ballot_w64(id != one) != 0) {  // not all of one document
+    r.any_lo = wave_min(id);
+    r.lo = wave_min(id < 0 ? INT32_MAX : id);
+    r.hi = wave_max(id < 0 ? -1 : id);
+  }
   return r;
 }
 
@@ -103,11 +104,14 @@ __device__ __forceinline__ float capped(const MaskedParams& p, float x) {
   return __builtin_fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
 }
 
-// Raw scores -> base-2 exponents, with the cap and the bias.  at: pos - first key of the tile - 4 hh of this lane.
-// small (the same in the whole wavefront): no raw score exceeds p.small, and the cap is a polynomial: five instructions a score
-// instead of three and an exponential and a reciprocal, which take four times as long each.
+// Raw scores -> scores whose product with the kernel's c is the base-2 exponent (c is 1 with a cap, else |scale| log2 e).
+// at: pos - first key of the tile - 4 hh of this lane;  slope: slope log2(e) / c.
+// small (the same in the whole wavefront): the largest scores of the rows are at most p.small in absolute value, and the cap is a
+// polynomial that is increasing throughout: four instructions a score instead of three and an exponential and a reciprocal, which
+// take four times as long each.  (Scores under -p.small are off by more, 1e-5 of themselves at 1.6 times that, but their
+// probabilities are small against that of their row's largest.)
 template <int NKB, bool CAP, bool BIAS>
-__device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParams& p, bool small, float slope_log2, int at) {
+__device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParams& p, bool small, float slope, int at) {
   if constexpr (CAP) {
     if (small) {
 #pragma unroll
@@ -115,7 +119,7 @@ __device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParam
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float x = s[kb][i], z = x * x;
-          s[kb][i] = x * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, p.poly[3], p.poly[2]), p.poly[1]), p.poly[0]);
+          s[kb][i] = x * __builtin_fmaf(z, __builtin_fmaf(z, p.poly[2], p.poly[1]), p.poly[0]);
         }
     } else {
 #pragma unroll
@@ -129,10 +133,7 @@ __device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParam
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = CAP ? s[kb][i] : s[kb][i] * p.c_true;
-        s[kb][i] = __builtin_fmaf(-slope_log2, __builtin_fabsf(base - (float)key_of(kb, i)), x);
-      }
+      for (int i = 0; i < 16; ++i) s[kb][i] = __builtin_fmaf(-slope, __builtin_fabsf(base - (float)key_of(kb, i)), s[kb][i]);
   }
 }
 
@@ -351,14 +352,36 @@ __device__ __forceinline__ void store_rows(const MaskedParams& p, const Lane<T>&
   }
 }
 
+// slope * KEY + start, the constant within the instruction: as an operand the compiler keeps all 32 of a lane in registers.
+template <int KEY>
+__device__ __forceinline__ float linear_at(float slope, float start) {
+  float x;
+  asm("v_fmamk_f32 %0, %1, %3, %2" : "=v"(x) : "v"(slope), "v"(start), "n"(__builtin_bit_cast(int, (float)KEY)));
+  return x;
+}
+template <int NKB>
+__device__ __forceinline__ void linear_scores(f32x16 (&s)[NKB], float slope, float start) {
+  static_for<0, NKB * 16>([&](auto kc) {
+    constexpr int k = decltype(kc)::value;
+    s[k / 16][k % 16] = linear_at<key_of(k / 16, k % 16)>(slope, start);
+  });
+}
+
+// What a step does beside the softmax of an unmasked tile.
+enum class Shape : int {
+  kNone,
+  kCap,     // sc are raw scores; their exponent is sc * (poly[0] + poly[1] sc^2 + poly[2] sc^4) - mc, see shape_scores
+  kLinear,  // a bias that is linear over the tile: the accumulators of S^T(t+1) hold slope * key + start already, and those of
+            // S^T(t), once their exponentials are taken, get what S^T(t+2) begins with
+};
+
 // One step: the exponentials of tile t beside the MFMAs of S^T(t+1) = K(t+1) Q^T and of O^T += V(t)^T P(t)^T, in the slots of
-// tile_step (attn_device.h), then the maximum of S^T(t+1), with ABS also of its absolute values.
-//   POLY: the exponent of a score is sc * (poly[0] + .. sc^6) - mc: small raw scores of a cap are shaped here (see shape_scores).
+// tile_step (attn_device.h), then the maximum of S^T(t+1).
 //   LSE: lx takes the sum of the fp32 probabilities.      issue: called behind every MFMA, for the loads of later tiles.
-template <class T, int KOFF, int VOFF, int PD, bool POLY, bool ABS, bool LSE, class Issue>
+template <class T, int KOFF, int VOFF, int PD, Shape SHAPE, bool LSE, class Issue>
 __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int (&ka_)[T::NKS], uint32_t (&pb)[T::NKB][8], const bf16x8 (&qf)[T::NKS],
                                             f32x16 (&o)[T::NDB], f32x16 (&sc)[T::NKB], f32x16 (&sn)[T::NKB], float c, float mc,
-                                            const float (&poly)[4], float& mx, float& am, float& lx, Issue&& issue) {
+                                            const float (&poly)[3], float slope, float start, float& mx, float& lx, Issue&& issue) {
   using S = StepSlots<T>;
   constexpr int NQ = T::NQK, N = S::N;
   static_assert(T::NKB == 2, "two key blocks per tile");
@@ -384,7 +407,7 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
       o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[J % PD], __builtin_bit_cast(bf16x8, pw), o[db], 0, 0, 0);
     } else {
       constexpr int ks = J / T::NKB, kb = J % T::NKB;
-      if constexpr (ks == 0) {
+      if constexpr (ks == 0 && SHAPE != Shape::kLinear) {
         const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         sn[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[J % PD], qf[ks], zero, 0, 0, 0);
       } else {
@@ -393,9 +416,9 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
     }
   };
   auto exponent = [&](float x) {
-    if constexpr (POLY) {
+    if constexpr (SHAPE == Shape::kCap) {
       const float z = x * x;
-      return __builtin_fmaf(x, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, poly[3], poly[2]), poly[1]), poly[0]), -mc);
+      return __builtin_fmaf(x, __builtin_fmaf(z, __builtin_fmaf(z, poly[2], poly[1]), poly[0]), -mc);
     } else {
       return __builtin_fmaf(x, c, -mc);
     }
@@ -408,6 +431,10 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
       constexpr int kb = k / 8, i = 2 * (k % 8);
       f0 = __builtin_amdgcn_exp2f(exponent(sc[kb][i]));
       f1 = __builtin_amdgcn_exp2f(exponent(sc[kb][i + 1]));
+      if constexpr (SHAPE == Shape::kLinear) {
+        sc[kb][i] = linear_at<key_of(kb, i)>(slope, start);
+        sc[kb][i + 1] = linear_at<key_of(kb, i + 1)>(slope, start);
+      }
     }
     if constexpr (k > 0) {
       SCHED_FENCE();
@@ -430,24 +457,15 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
     issue(jc);
     if constexpr (J >= S::max_slot0) {
       constexpr int m = J - S::max_slot0, kb = m / 2, i = 8 * (m % 2);
-#define DIT_MAX(out, first, open, close)                                                                                                    \
-  if constexpr (first)                                                                                                                      \
-    asm("v_max3_f32 %0, " open "%1" close ", " open "%2" close ", " open "%3" close "\n\tv_max3_f32 %0, %0, " open "%4" close ", " open   \
-        "%5" close "\n\tv_max3_f32 %0, %0, " open "%6" close ", " open "%7" close "\n\tv_max_f32 %0, %0, " open "%8" close               \
-        : "=&v"(out)                                                                                                                        \
-        : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),               \
-          "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]));                                                                                          \
-  else                                                                                                                                      \
-    asm("v_max3_f32 %0, %0, " open "%1" close ", " open "%2" close "\n\tv_max3_f32 %0, %0, " open "%3" close ", " open "%4" close         \
-        "\n\tv_max3_f32 %0, %0, " open "%5" close ", " open "%6" close "\n\tv_max3_f32 %0, %0, " open "%7" close ", " open "%8" close    \
-        : "+v"(out)                                                                                                                         \
-        : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),               \
-          "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]))
-      DIT_MAX(mx, m == 0, "", "");
-      if constexpr (ABS) {
-        DIT_MAX(am, m == 0, "|", "|");
-      }
-#undef DIT_MAX
+      if constexpr (m == 0)
+        asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max_f32 %0, %0, %8"
+            : "=&v"(mx)
+            : "v"(sn[0][0]), "v"(sn[0][1]), "v"(sn[0][2]), "v"(sn[0][3]), "v"(sn[0][4]), "v"(sn[0][5]), "v"(sn[0][6]), "v"(sn[0][7]));
+      else
+        asm("v_max3_f32 %0, %0, %1, %2\n\tv_max3_f32 %0, %0, %3, %4\n\tv_max3_f32 %0, %0, %5, %6\n\tv_max3_f32 %0, %0, %7, %8"
+            : "+v"(mx)
+            : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),
+              "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]));
     }
     SCHED_FENCE();
   });
@@ -555,7 +573,8 @@ masked_attn_kernel(MaskedParams p) {
     const int kv_head = it.head / p.group;
     const char* kbase = static_cast<const char*>(p.k) + (int64_t)it.kv_start * p.k_stride_b + (int64_t)kv_head * T::ROW_B;
     const char* vbase = static_cast<const char*>(p.v) + (int64_t)it.kv_start * p.v_stride_b + (int64_t)kv_head * T::ROW_B;
-    const float slope = BIAS ? p.slopes[it.head] * 1.44269504088896340736f : 0.f;
+    const float c = CAP ? 1.f : p.c_log2;
+    const float slope = BIAS ? p.slopes[it.head] * 1.44269504088896340736f / c : 0.f;
     const uint32_t lds_wave = lds + (uint32_t)wave * 1024u;
     const TailRows tail = tail_rows<T>(lim);
     uint32_t kvoff, vvoff;
@@ -613,18 +632,18 @@ masked_attn_kernel(MaskedParams p) {
     fresh_lane().operand_addrs(lds, lds, ka, va);
     int turn = 0;  // of the bad-key masks
     bool poison = false;
-    float mx = 0.f, am = 0.f;
+    float mx = 0.f;
     f32x16 sa[T::NKB], sb[T::NKB];
     uint32_t pb[T::NKB][8];
-    const float c = CAP || BIAS ? 1.f : p.c_log2;
 
-    // Scores of tile t, from S^T to base-2 exponents with the dead ones -inf, and their maximum mx.  Before, mx (and am) are
-    // those of the raw scores; the cap is monotonic, so the capped maximum is that of the raw one.
-    auto is_small = [&]() { return CAP && __builtin_amdgcn_ballot_w64(am > p.small) == 0; };
+    // Scores of tile t, from S^T to shaped ones with the dead ones -inf, and their maximum mx.  Before, mx is that of the raw
+    // scores; the cap is monotonic, so the capped maximum is that of the raw one.
+    auto is_small = [&]() { return __builtin_amdgcn_ballot_w64(!(__builtin_fabsf(mx) <= p.small)) == 0; };
+    // pos - first key of tile t - 4 hh
+    auto distance = [&](int t) { return pos0 + query_row() - tile_first_key<T>(t, lim) - 4 * half_of(tid); };
     auto finish = [&](f32x16(&s)[T::NKB], int t, int slot, bool masked) {
       const int key0 = tile_first_key<T>(t, lim);
-      if constexpr (CAP || BIAS)
-        shape_scores<T::NKB, CAP, BIAS>(s, p, is_small(), slope, BIAS ? pos0 + query_row() - key0 - 4 * half_of(tid) : 0);
+      if constexpr (CAP || BIAS) shape_scores<T::NKB, CAP, BIAS>(s, p, CAP && is_small(), slope, BIAS ? distance(t) : 0);
       if (masked) {
         int doc;
         const int hh = half_of(tid), klim = row_mask(query_row(), doc);
@@ -684,7 +703,6 @@ masked_attn_kernel(MaskedParams p) {
     mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, sa);
     scores_ready<T>(sa);
     mx = tile_max<T>(sa);
-    am = __builtin_inff();  // the first tile's cap is not the polynomial
 
     // Tiles under free_end need no mask but for ids.  In a run of such tiles, whose ids agree too, a step has no tests and loads
     // from running pointers, spread behind its MFMAs.
@@ -693,26 +711,30 @@ masked_attn_kernel(MaskedParams p) {
     static_assert(EVERY >= 1, "a step's loads fit its slots");
     const char *kp = kbase, *vp = vbase;
     const int64_t k_step = (int64_t)T::BN * p.k_stride_b, v_step = (int64_t)T::BN * p.v_stride_b;
-    // A step from t (scores raw with POLY, else finished, in sc; K(t + 1) and V(t) on their way) to t + 1 (raw, in sn).
+    constexpr Shape SHAPE = BIAS ? (CAP ? Shape::kNone : Shape::kLinear) : CAP ? Shape::kCap : Shape::kNone;
+    // With kLinear all keys of a run lie on one side of all rows, and its bias is side * (key - pos).
+    float side = 0.f;
+    // A step from t (scores raw with kCap, else shaped, in sc; K(t + 1) and V(t) on their way) to t + 1 (in sn, shaped with
+    // kLinear, else raw).
     auto run_step = [&](auto uc, f32x16(&sc)[T::NKB], f32x16(&sn)[T::NKB]) {
       constexpr int U = decltype(uc)::value;
-      constexpr bool POLY = CAP && !BIAS;
       wait_loads();
       wg_barrier();
-      float poly[4] = {1.f, 0.f, 0.f, 0.f};
-      if constexpr (POLY) {
-        mx = capped(p, mx);
+      float poly[3] = {1.f, 0.f, 0.f};
+      if constexpr (SHAPE == Shape::kCap) {
         if (is_small()) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) poly[i] = p.poly[i];
+          for (int i = 0; i < 3; ++i) poly[i] = p.poly[i];
         } else {
           shape_scores<T::NKB, CAP, false>(sc, p, false, 0.f, 0);
         }
+        mx = capped(p, mx);
       }
+      const float start = SHAPE == Shape::kLinear ? -side * (float)distance(t0 + 2) : 0.f;
       raise();
       const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
-      masked_step<T, (1 - U) * T::TILE_B, U * T::TILE_B, kPrefetch, POLY, CAP, LSE>(
-          va, ka, pb, qf, o, sc, sn, c, mc, poly, mx, am, r.lx, [&](auto jc) {
+      masked_step<T, (1 - U) * T::TILE_B, U * T::TILE_B, T::D == 64 && SHAPE == Shape::kLinear ? 3 : kPrefetch, SHAPE, LSE>(
+          va, ka, pb, qf, o, sc, sn, c, mc, poly, side, start, mx, r.lx, [&](auto jc) {
             constexpr int J = decltype(jc)::value;
             if constexpr (J % EVERY == EVERY / 2 && J / EVERY < NLOAD) {
               constexpr int j = J / EVERY, i = j % T::LPT;
@@ -740,28 +762,40 @@ masked_attn_kernel(MaskedParams p) {
     };
     while (t1 < tiles.end) {
       // Here the scores of t0 are raw, in sa; K(t1) and V(t0) are on their way.
+      bool shaped = false;
       if (slot == 0 && !masked0) {
         int run_end = free_end;
         if (tiles.ranges != nullptr) {
           const int rest = t0 >= tiles.base ? t0 + (int)__builtin_ctzll(~((tiles.live & tiles.pure) >> (t0 - tiles.base)) | 1ull << 63) : t0;
           run_end = rest < run_end ? rest : run_end;
         }
+        if constexpr (SHAPE == Shape::kLinear) {
+          const int left_end = pos0 >= 0 ? (pos0 + 1) / T::BN : 0;  // tiles whose keys are all up to the first row's place
+          const bool right = t0 * T::BN >= pos0 + it.q_rows - 1;    // all from the last one's on
+          side = right ? -slope : slope;
+          if (!right && left_end < run_end) run_end = left_end;
+        }
         if (t0 + 3 < run_end) {
           kp = kbase + (int64_t)(t0 + 2) * k_step;
           vp = vbase + (int64_t)(t0 + 1) * v_step;
+          if constexpr (SHAPE == Shape::kLinear) {
+            finish(sa, t0, 0, false);
+            linear_scores<T::NKB>(sb, side, -side * (float)distance(t0 + 1));
+          }
           do {
-            if constexpr (BIAS) finish(sa, t0, 0, false);
+            if constexpr (SHAPE == Shape::kNone && BIAS) finish(sa, t0, 0, false);
             run_step(IC<0>{}, sa, sb);
-            if constexpr (BIAS) finish(sb, t0, 0, false);
+            if constexpr (SHAPE == Shape::kNone && BIAS) finish(sb, t0, 0, false);
             run_step(IC<1>{}, sb, sa);
           } while (t0 + 3 < run_end);
+          shaped = SHAPE == Shape::kLinear;
           t1 = t0 + 1;
           t2 = tiles.next(t1 + 1);
           masked0 = masked1 = false;
           masked2 = t2 < tiles.end && needs_mask(t2);
         }
       }
-      finish(sa, t0, slot, masked0);
+      if (!shaped) finish(sa, t0, slot, masked0);
       const int t3 = tiles.next(t2 + 1);
       const bool masked3 = t3 < tiles.end && needs_mask(t3);
       wait_loads();
@@ -773,7 +807,7 @@ masked_attn_kernel(MaskedParams p) {
       raise();
       const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
       turn_k();
-      masked_step<T, 0, 0, kPrefetch, false, CAP, LSE>(va, ka, pb, qf, o, sa, sb, c, mc, p.poly, mx, am, r.lx, [](auto) {});
+      masked_step<T, 0, 0, kPrefetch, Shape::kNone, LSE>(va, ka, pb, qf, o, sa, sb, c, mc, p.poly, 0.f, 0.f, mx, r.lx, [](auto) {});
       turn_slots();
       r.l += row_sum<T>(pb);
       asm volatile("" : "+v"(r.l));
@@ -810,7 +844,7 @@ masked_attn_kernel(MaskedParams p) {
   if constexpr (LSE) {
     const int qrow = wave * 32 + (tid & 31);
     if (qrow < it.q_rows && (tid & 32) == 0) {
-      const float c = CAP || BIAS ? 1.f : p.c_log2;
+      const float c = CAP ? 1.f : p.c_log2;
       float* dst = part_row >= 0 ? p.part_lse + (part_row + qrow) * n_heads : p.lse + (int64_t)(it.q_start + qrow) * n_heads;
       if (part_row >= 0 || p.lse != nullptr) dst[it.head] = any ? kLn2 * (r.m_ref * c + __builtin_amdgcn_logf(lx)) : -__builtin_inff();
     }
@@ -917,7 +951,7 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_wav
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   RowState r = {kNoReference, 0.f, 0.f};
-  const float c = CAP || BIAS ? 1.f : p.c_log2;
+  const float c = CAP ? 1.f : p.c_log2;
   const uint32_t kbuf = lds + (uint32_t)wave * F::WAVE_B, vbuf = kbuf + F::BLOCK_B, docs = lds + F::DOCS_OFF + (uint32_t)wave * (2 * F::DOCS_B);
 
   int block = t0 < tiles.end ? next_block(first_block) : n_blocks;
@@ -926,7 +960,7 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_wav
     const char* vbase = static_cast<const char*>(p.v) + (int64_t)sq.kv_start * p.v_stride_b + (int64_t)kv_head * T::ROW_B;
     int head;
     const int row = column(head);
-    const float slope = BIAS ? p.slopes[head] * 1.44269504088896340736f : 0.f;
+    const float slope = BIAS ? p.slopes[head] * 1.44269504088896340736f / c : 0.f;
     const int at0 = BIAS ? pos0 + row - 4 * hh : 0;
     // Lane offsets of the load instructions, RPI rows each: a V row's chunk order has a period of one, a K row's of KN.
     constexpr int KN = 16 / T::RPI;
