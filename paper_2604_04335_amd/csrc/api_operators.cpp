@@ -304,10 +304,13 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
     // tanh(x) / x as a polynomial in x^2, off by at most 4e-7 relative for |x| <= 0.25 (a fit of least maximal error).
     const double a[3] = {0.9999996043443452, -0.33321908223103114, 0.12841613400294474};
     const double k = std::fabs(static_cast<double>(scale)) / m.softcap;
-    p.small = static_cast<float>(0.25 / k);  // scale 0: infinite
+    // (Finite with scale 0, so that an infinite score is not among them, and with a finite square.)
+    p.poly_up_to = static_cast<float>(std::min(0.25 / k, 1e18));
+    // Exponents of at most 30 either way.
+    p.small = std::min(p.poly_up_to, static_cast<float>(30.0 / (1.44269504088896340736 * std::fabs(static_cast<double>(scale)))));
     for (int i = 0; i < 3; ++i) {
       p.poly[i] = static_cast<float>(a[i] * m.softcap * 1.44269504088896340736 * std::pow(k, 2 * i + 1));
-      if (!std::isfinite(p.poly[i])) p.small = -1.f;  // never
+      if (!std::isfinite(p.poly[i])) p.small = p.poly_up_to = -1.f;  // never
     }
   }
   p.q_stride_b = 2 * strides[0];

@@ -36,7 +36,8 @@ struct MaskedParams : AttnParams {
   const float* slopes;     // [n_heads] or nullptr
   float tanh_in;           // 2 * log2(e) * |scale| / cap
   float cap_log2;          // cap * log2(e)
-  float small, poly[3];    // cap: raw scores up to `small` take s (poly[0] + poly[1] s^2 + poly[2] s^4)
+  float poly_up_to, poly[3];  // cap: raw scores up to it are s (poly[0] + poly[1] s^2 + poly[2] s^4)
+  float small;                // and where it is at most this, the largest absolute value of a row stands in for its maximum
   int32_t causal;
   int32_t group;           // query heads per key head
   int32_t part_tiles;      // 64-key tiles of a part

@@ -98,18 +98,22 @@ struct LiveTiles {
 // Scores of a lane: element i of block kb is key 32 kb + 8 (i / 4) + (i % 4) + 4 hh of the tile.
 __device__ __forceinline__ constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i >> 2) + (i & 3); }
 
-// C tanh(s / C) log2(e) of a raw score: tanh y = 1 - 2 / (exp(2 y) + 1), whose limits need no clamp.
+// C tanh(s / C) log2(e) of a raw score, as a polynomial where it is small and 1 - 2 / (exp(2 y) + 1) of y = s / C, whose limits
+// need no clamp, where that keeps its relative precision.
+__device__ __forceinline__ float small_cap(const MaskedParams& p, float x) {
+  const float z = x * x;
+  return x * __builtin_fmaf(z, __builtin_fmaf(z, p.poly[2], p.poly[1]), p.poly[0]);
+}
 __device__ __forceinline__ float capped(const MaskedParams& p, float x) {
   const float e = __builtin_amdgcn_exp2f(x * p.tanh_in);
-  return __builtin_fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
+  const float large = __builtin_fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
+  return __builtin_fabsf(x) <= p.poly_up_to ? small_cap(p, x) : large;
 }
 
 // Raw scores -> scores whose product with the kernel's c is the base-2 exponent (c is 1 with a cap, else |scale| log2 e).
 // at: pos - first key of the tile - 4 hh of this lane;  slope: slope log2(e) / c.
-// small (the same in the whole wavefront): the largest scores of the rows are at most p.small in absolute value, and the cap is a
-// polynomial that is increasing throughout: four instructions a score instead of three and an exponential and a reciprocal, which
-// take four times as long each.  (Scores under -p.small are off by more, 1e-5 of themselves at 1.6 times that, but their
-// probabilities are small against that of their row's largest.)
+// small (the same in the whole wavefront): no score exceeds p.small in absolute value, and the cap is the polynomial alone: four
+// instructions a score instead of nine and an exponential and a reciprocal, which take four times as long each.
 template <int NKB, bool CAP, bool BIAS>
 __device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParams& p, bool small, float slope, int at) {
   if constexpr (CAP) {
@@ -117,10 +121,7 @@ __device__ __forceinline__ void shape_scores(f32x16 (&s)[NKB], const MaskedParam
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = s[kb][i], z = x * x;
-          s[kb][i] = x * __builtin_fmaf(z, __builtin_fmaf(z, p.poly[2], p.poly[1]), p.poly[0]);
-        }
+        for (int i = 0; i < 16; ++i) s[kb][i] = small_cap(p, s[kb][i]);
     } else {
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -376,9 +377,9 @@ enum class Shape : int {
 };
 
 // One step: the exponentials of tile t beside the MFMAs of S^T(t+1) = K(t+1) Q^T and of O^T += V(t)^T P(t)^T, in the slots of
-// tile_step (attn_device.h), then the maximum of S^T(t+1).
+// tile_step (attn_device.h), then the maximum of S^T(t+1), with ABS that of its absolute values.
 //   LSE: lx takes the sum of the fp32 probabilities.      issue: called behind every MFMA, for the loads of later tiles.
-template <class T, int KOFF, int VOFF, int PD, Shape SHAPE, bool LSE, class Issue>
+template <class T, int KOFF, int VOFF, int PD, Shape SHAPE, bool ABS, bool LSE, class Issue>
 __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int (&ka_)[T::NKS], uint32_t (&pb)[T::NKB][8], const bf16x8 (&qf)[T::NKS],
                                             f32x16 (&o)[T::NDB], f32x16 (&sc)[T::NKB], f32x16 (&sn)[T::NKB], float c, float mc,
                                             const float (&poly)[3], float slope, float start, float& mx, float& lx, Issue&& issue) {
@@ -457,15 +458,24 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
     issue(jc);
     if constexpr (J >= S::max_slot0) {
       constexpr int m = J - S::max_slot0, kb = m / 2, i = 8 * (m % 2);
-      if constexpr (m == 0)
-        asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max_f32 %0, %0, %8"
-            : "=&v"(mx)
-            : "v"(sn[0][0]), "v"(sn[0][1]), "v"(sn[0][2]), "v"(sn[0][3]), "v"(sn[0][4]), "v"(sn[0][5]), "v"(sn[0][6]), "v"(sn[0][7]));
-      else
-        asm("v_max3_f32 %0, %0, %1, %2\n\tv_max3_f32 %0, %0, %3, %4\n\tv_max3_f32 %0, %0, %5, %6\n\tv_max3_f32 %0, %0, %7, %8"
-            : "+v"(mx)
-            : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),
-              "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]));
+#define DIT_MAX(O, C)                                                                                                               \
+  if constexpr (m == 0)                                                                                                              \
+    asm("v_max3_f32 %0, " O "%1" C ", " O "%2" C ", " O "%3" C "\n\tv_max3_f32 %0, %0, " O "%4" C ", " O "%5" C                    \
+        "\n\tv_max3_f32 %0, %0, " O "%6" C ", " O "%7" C "\n\tv_max3_f32 %0, %0, %0, " O "%8" C                                  \
+        : "=&v"(mx)                                                                                                                  \
+        : "v"(sn[0][0]), "v"(sn[0][1]), "v"(sn[0][2]), "v"(sn[0][3]), "v"(sn[0][4]), "v"(sn[0][5]), "v"(sn[0][6]), "v"(sn[0][7]));  \
+  else                                                                                                                               \
+    asm("v_max3_f32 %0, %0, " O "%1" C ", " O "%2" C "\n\tv_max3_f32 %0, %0, " O "%3" C ", " O "%4" C                              \
+        "\n\tv_max3_f32 %0, %0, " O "%5" C ", " O "%6" C "\n\tv_max3_f32 %0, %0, " O "%7" C ", " O "%8" C                        \
+        : "+v"(mx)                                                                                                                   \
+        : "v"(sn[kb][i]), "v"(sn[kb][i + 1]), "v"(sn[kb][i + 2]), "v"(sn[kb][i + 3]), "v"(sn[kb][i + 4]), "v"(sn[kb][i + 5]),        \
+          "v"(sn[kb][i + 6]), "v"(sn[kb][i + 7]))
+      if constexpr (ABS) {
+        DIT_MAX("|", "|");
+      } else {
+        DIT_MAX("", "");
+      }
+#undef DIT_MAX
     }
     SCHED_FENCE();
   });
@@ -636,14 +646,16 @@ masked_attn_kernel(MaskedParams p) {
     f32x16 sa[T::NKB], sb[T::NKB];
     uint32_t pb[T::NKB][8];
 
-    // Scores of tile t, from S^T to shaped ones with the dead ones -inf, and their maximum mx.  Before, mx is that of the raw
-    // scores; the cap is monotonic, so the capped maximum is that of the raw one.
-    auto is_small = [&]() { return __builtin_amdgcn_ballot_w64(!(__builtin_fabsf(mx) <= p.small)) == 0; };
+    // Scores of tile t, from S^T to shaped ones with the dead ones -inf, and their maximum mx.  Before, mx is the maximum of the
+    // raw scores, with a cap that of their absolute values: if it is small, its capped value serves as the maximum, which it
+    // exceeds by at most 2^60 in the probabilities (p.small); else the shaped scores are gone through.
+    auto is_small = [&]() { return __builtin_amdgcn_ballot_w64(!(mx <= p.small)) == 0; };
     // pos - first key of tile t - 4 hh
     auto distance = [&](int t) { return pos0 + query_row() - tile_first_key<T>(t, lim) - 4 * half_of(tid); };
     auto finish = [&](f32x16(&s)[T::NKB], int t, int slot, bool masked) {
       const int key0 = tile_first_key<T>(t, lim);
-      if constexpr (CAP || BIAS) shape_scores<T::NKB, CAP, BIAS>(s, p, CAP && is_small(), slope, BIAS ? distance(t) : 0);
+      const bool small = CAP && is_small();
+      if constexpr (CAP || BIAS) shape_scores<T::NKB, CAP, BIAS>(s, p, small, slope, BIAS ? distance(t) : 0);
       if (masked) {
         int doc;
         const int hh = half_of(tid), klim = row_mask(query_row(), doc);
@@ -651,11 +663,11 @@ masked_attn_kernel(MaskedParams p) {
         const LaneMask m = {lo - 4 * hh, n > 0 ? (unsigned)n : 0u};
         mask_scores<T::NKB>(s, m, have_docs, lds + kDocsOff<T> + slot * (T::BN * 4), doc, hh);
       }
-      if (BIAS || masked) {
+      if (BIAS || masked || (CAP && !small)) {
         scores_ready<T>(s);
         mx = tile_max<T>(s);
       } else if constexpr (CAP) {
-        mx = capped(p, mx);
+        mx = small_cap(p, mx);
       }
     };
     // Behind the loads of V of a masked tile, before the barrier: this wavefront's rows of it become finite.
@@ -701,8 +713,12 @@ masked_attn_kernel(MaskedParams p) {
 
     if (t1 < tiles.end) load_k(t1, 1);
     mfma_stream<T, false, 0, T::NQK, kPrefetch>(smem, va, ka, pb, qf, o, sa);
-    scores_ready<T>(sa);
-    mx = tile_max<T>(sa);
+    if constexpr (CAP) {
+      mx = __builtin_inff();  // not known of the first tile
+    } else {
+      scores_ready<T>(sa);
+      mx = tile_max<T>(sa);
+    }
 
     // Tiles under free_end need no mask but for ids.  In a run of such tiles, whose ids agree too, a step has no tests and loads
     // from running pointers, spread behind its MFMAs.
@@ -725,15 +741,17 @@ masked_attn_kernel(MaskedParams p) {
         if (is_small()) {
 #pragma unroll
           for (int i = 0; i < 3; ++i) poly[i] = p.poly[i];
+          mx = small_cap(p, mx);
         } else {
           shape_scores<T::NKB, CAP, false>(sc, p, false, 0.f, 0);
+          scores_ready<T>(sc);
+          mx = tile_max<T>(sc);
         }
-        mx = capped(p, mx);
       }
       const float start = SHAPE == Shape::kLinear ? -side * (float)distance(t0 + 2) : 0.f;
       raise();
       const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
-      masked_step<T, (1 - U) * T::TILE_B, U * T::TILE_B, T::D == 64 && SHAPE == Shape::kLinear ? 3 : kPrefetch, SHAPE, LSE>(
+      masked_step<T, (1 - U) * T::TILE_B, U * T::TILE_B, T::D == 64 && SHAPE == Shape::kLinear ? 3 : kPrefetch, SHAPE, CAP, LSE>(
           va, ka, pb, qf, o, sc, sn, c, mc, poly, side, start, mx, r.lx, [&](auto jc) {
             constexpr int J = decltype(jc)::value;
             if constexpr (J % EVERY == EVERY / 2 && J / EVERY < NLOAD) {
@@ -807,7 +825,7 @@ masked_attn_kernel(MaskedParams p) {
       raise();
       const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
       turn_k();
-      masked_step<T, 0, 0, kPrefetch, Shape::kNone, LSE>(va, ka, pb, qf, o, sa, sb, c, mc, p.poly, 0.f, 0.f, mx, r.lx, [](auto) {});
+      masked_step<T, 0, 0, kPrefetch, Shape::kNone, CAP, LSE>(va, ka, pb, qf, o, sa, sb, c, mc, p.poly, 0.f, 0.f, mx, r.lx, [](auto) {});
       turn_slots();
       r.l += row_sum<T>(pb);
       asm volatile("" : "+v"(r.l));

@@ -290,6 +290,26 @@ def test_masked_scales(ctx, i, scale):
     _check_masked(out, lse, q, k, v, cu_q, cu_k, scale, **kw)
 
 
+@pytest.mark.parametrize("cap,low,high", [(5.0, -6.0, 0.5), (5.0, -30.0, -3.0), (50.0, -20.0, 2.0), (500.0, -300.0, -90.0), (2.0, -1e4, 0.1), (1e6, -400.0, 400.0)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_capped_scores_far_from_their_row_largest(ctx, cap, low, high, D):
+    """Nearly all scores of a row near `low`, a few near `high`, in every tile or in the first, a middle or the last one only."""
+    rng = _rng(D + int(cap))
+    n, H = 700, 1
+    u = rng.standard_normal(D)
+    u /= np.linalg.norm(u)
+    scale = 0.125
+    q = f32_to_bf16_bits((8.0 * u[None, None] + 0.05 * rng.standard_normal((n, H, D))).astype(np.float32))
+    level = np.full(n, low)
+    level[rng.integers(0, n, 5)] = high
+    level[[3, 350, 699]] = high
+    k = f32_to_bf16_bits((level[:, None, None] * u[None, None] + 0.05 * rng.standard_normal((n, H, D))).astype(np.float32))
+    v = _bf16(rng, n, H, D)
+    cu = _cu([n])
+    out, lse = _run_masked(ctx, to_dev(q), to_dev(k), to_dev(v), cu, None, scale, da.AttnMask(softcap=cap))
+    _check_masked(out, lse, q, k, v, cu, cu, scale, cap=cap)
+
+
 @pytest.mark.parametrize("few,D,parts", [(False, 64, False), (False, 128, False), (False, 128, True), (True, 64, False), (True, 128, True)])
 def test_what_a_row_does_not_see_has_no_effect(ctx, few, D, parts):
     """NaN and infinite keys and values behind a causal mask: rows before them keep their bits, rows that see them get them."""
