@@ -55,7 +55,7 @@ extern "C" {
 #define DIT_ATTN_ERR_MASK          (-13) /* dit_attn_mask: a field out of range, or one without the one it belongs to */
 #define DIT_ATTN_ERR_ROPE          (-14) /* dit_attn_rope, rot_dim or layout out of range */
 #define DIT_ATTN_ERR_NORM          (-15) /* no such norm, eps out of range, or weights without a norm */
-#define DIT_ATTN_ERR_STRIDE        (-16) /* a row stride that is no multiple of 8, too short for a row or too long */
+#define DIT_ATTN_ERR_STRIDE        (-16) /* a row stride that is no multiple of 8, too short for a row or too long; one side's rows are the other's */
 
 typedef struct dit_attn_ctx dit_attn_ctx; /* opaque */
 

@@ -134,7 +134,8 @@ class NormHeads(ctypes.Structure):
         if n_heads is None:
             n_heads = x.shape[1]
         super().__init__(_ptr(x), _ptr(out), _row_stride(x, "x") if row_stride is None else int(row_stride),
-                         _row_stride(out, "out") if out_row_stride is None else int(out_row_stride), _ptr(weight), _ptr(bias), int(n_heads))
+                         _row_stride(out, "out") if out_row_stride is None else int(out_row_stride), _array(weight, "weight", True),
+                         _array(bias, "bias", True), int(n_heads))
         self._held = (x, out, weight, bias)
 
 
@@ -150,7 +151,8 @@ class AttnMask(ctypes.Structure):
             prefix = [int(x) for x in prefix]
             self.n_prefix = len(prefix)
             prefix = (ctypes.c_int32 * max(len(prefix), 1))(*prefix)
-        super().__init__(int(causal), float(softcap), prefix, _ptr(slopes), _ptr(q_doc), _ptr(k_doc))
+        super().__init__(int(causal), float(softcap), prefix, _array(slopes, "slopes", True), _array(q_doc, "q_doc", False),
+                         _array(k_doc, "k_doc", False))
         self._held = (prefix, slopes, q_doc, k_doc)
 
 
@@ -248,6 +250,14 @@ def _row_stride(x, name: str) -> int:
         if (inner == 1 or shape[2] == 1) and (heads == shape[2] or shape[1] == 1):
             return rows if shape[0] > 1 else 0
     raise ValueError(f"{name}: a bf16 tensor [rows, heads, head_dim] whose heads are contiguous")
+
+
+def _array(x, name: str, floating: bool) -> int:
+    """Address of a contiguous device array of 4-byte floats or integers; a tensor of another kind is refused."""
+    if x is not None and hasattr(x, "element_size"):
+        if x.element_size() != 4 or x.is_floating_point() != floating or not x.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {'fp32' if floating else 'int32'} tensor")
+    return _ptr(x)
 
 
 def _cu_array(cu_seqlens) -> np.ndarray:
@@ -416,7 +426,8 @@ def dit_attn_sp_unpack_heads(ctx, src, dst, n_rows: int, n_heads: int, head_dim:
 
 def dit_attn_rope_table(ctx, positions, n_rows: int, rope: RopeSpec, table, stream=None) -> None:
     """table[r, pair] = (cos, sin) of the row's positions; positions: device int32 [n_rows, n_axes]; see include/dit_attn.h."""
-    rc = load_library().dit_attn_rope_table(ctx, _ptr(positions), n_rows, rope, _ptr(table), _ptr(stream))
+    rc = load_library().dit_attn_rope_table(ctx, _array(positions, "positions", False), n_rows, rope, _array(table, "table", True),
+                                            _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 
@@ -424,7 +435,8 @@ def dit_attn_rope_table(ctx, positions, n_rows: int, rope: RopeSpec, table, stre
 def dit_attn_qk_norm_rope(ctx, q, k, n_rows: int, head_dim: int, norm: int, eps: float, table=None, rot_dim: int = 0,
                           layout: int = ROPE_INTERLEAVED, stream=None) -> None:
     """Norm of queries and keys for each head and rotation; q, k: NormHeads, or None for one of them; see include/dit_attn.h."""
-    rc = load_library().dit_attn_qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, _ptr(table), rot_dim, layout, _ptr(stream))
+    rc = load_library().dit_attn_qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, _array(table, "table", True), rot_dim, layout,
+                                              _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 
@@ -447,8 +459,10 @@ def dit_attn_masked_varlen_fwd(ctx, q, k, v, cu_seqlens_q, cu_seqlens_k, n_heads
         raise ValueError("mask.prefix needs an entry for every sequence")
     if row_strides is None:
         row_strides = (_row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v"))
+    if _row_stride(out, "out") != 0:
+        raise ValueError("out: contiguous rows")
     rc = lib.dit_attn_masked_varlen_fwd(ctx, _ptr(q), _ptr(k), _ptr(v), _I64x3(*row_strides), cq.__array_interface__["data"][0],
-                                        None if ck is None else ck.__array_interface__["data"][0], n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, _ptr(out), _ptr(lse), _ptr(stream))
+                                        None if ck is None else ck.__array_interface__["data"][0], n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, _ptr(out), _array(lse, "lse", True), _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 

@@ -20,6 +20,7 @@
 #include "merge.h"
 #include "noalloc.h"
 #include "plan.h"
+#include "qk_norm_rope.h"
 #include "sp_layout.h"
 
 namespace {
@@ -80,6 +81,7 @@ int dit_attn_create(dit_attn_ctx** out_ctx, int device_id) {
   // Kernel code resident and LDS limits set before the first launch; this device's fixed scratch resolved.
   if (e == hipSuccess) e = dit::attn_fwd_prepare();
   if (e == hipSuccess) e = dit::masked_attn_prepare();
+  if (e == hipSuccess) e = dit::qk_norm_rope_prepare();
   if (e == hipSuccess) e = dit::noalloc_init(device_id);
   if (e != hipSuccess) {
     (void)hipGetLastError();

@@ -143,6 +143,8 @@ int qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const dit_attn
     if (rc != DIT_ATTN_OK) return rc;
   }
   if (n_rows == 0) return DIT_ATTN_OK;
+  if (q && k && (q->out == k->out || q->out == k->x || k->out == q->x))
+    return fail(ctx, DIT_ATTN_ERR_STRIDE, "the output of one side is the other side's input or output");
   if (rot_dim > 0 && !table) return fail(ctx, DIT_ATTN_ERR_NULL, "table is NULL");
   if (rot_dim > 0 && misaligned(table, 16)) return fail(ctx, DIT_ATTN_ERR_ALIGN, "table must be 16-byte aligned");
   p.table = table;
@@ -299,7 +301,8 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   p.c_log2 = std::max(std::fabs(scale) * 1.44269504088896340736f, m.slopes ? 1e-20f : 1e-30f);
   p.negate = scale < 0.f ? 1 : 0;
   if (m.softcap > 0.f) {
-    p.tanh_in = static_cast<float>(2.0 * 1.44269504088896340736 * std::fabs(static_cast<double>(scale)) / m.softcap);
+    // Finite, so that a score of 0 times it is 0.
+    p.tanh_in = static_cast<float>(std::min(2.0 * 1.44269504088896340736 * std::fabs(static_cast<double>(scale)) / m.softcap, 3e38));
     p.cap_log2 = m.softcap * 1.44269504088896340736f;
     // tanh(x) / x as a polynomial in x^2, off by at most 4e-7 relative for |x| <= 0.25 (a fit of least maximal error).
     const double a[3] = {0.9999996043443452, -0.33321908223103114, 0.12841613400294474};

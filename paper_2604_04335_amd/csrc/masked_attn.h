@@ -50,6 +50,7 @@ struct MaskedKind {
   bool few_rows, cap, bias, lse;
 };
 
+// Loads the code of these kernels on the current device and sets their LDS limits.
 hipError_t masked_attn_prepare();
 // Doc tiles of the launch's sequences, then the attention kernel on p.n_items workgroups.
 hipError_t masked_attn_launch(const MaskedParams& p, const MaskedKind& kind, uint32_t n_doc_tiles, hipStream_t stream);

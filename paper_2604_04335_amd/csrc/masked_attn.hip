@@ -58,6 +58,8 @@ __device__ __forceinline__ DocTile doc_range(const int32_t* ids, int n) {
   return r;
 }
 
+// Id ranges of all key tiles of a launch, a wavefront each: 4 us with its launch, which spares the attention kernel the tiles of
+// other documents (two thirds of 6 x 4352 rows in three documents).
 __global__ void __launch_bounds__(256) masked_doc_tiles_kernel(MaskedParams p, uint32_t n_tiles) {
   const uint32_t tile = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (tile >= n_tiles) return;
@@ -484,7 +486,13 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
 }
 
 // The kernel works a tile ahead, as the unmasked 128-row kernel: the scores of the next tile are contracted beside the softmax of
-// this one.  What shapes and masks a tile's scores stands between two steps, for the tiles that need it.
+// this one.  Most tiles are touched by no mask; runs of them have a loop of their own, in which a cap and a bias cost their few
+// instructions a score beside the MFMAs.  What else shapes and masks a tile's scores stands between two steps.
+// us on MI355X, with the three parts of a tile in turn / now:  20506 rows x 24 heads, D 128, unmasked 5387 / 4330 (1190 TFLOP/s, the
+// unmasked 128-row kernel 4220), cap 6888 / 5060, bias 6237 / 4810, causal 2603 / 2130;  4352 x 24 x 6, D 64, unmasked 790 / 690,
+// bias 987 / 769, padded documents of three 559 / 412.  Bound by power (1.7 GHz) with both pipes of a SIMD over half busy; the
+// padded documents by vector instructions, half of their tiles being at an edge of a document or around the rows' own places.
+// 128 rows and not 64 or 256: two workgroups of four wavefronts fill a compute unit's registers and 130 of its 160 KB LDS.
 // Workgroups on a compute unit: what the registers allow.
 template <int D, bool CAP, bool LSE>
 constexpr int kMaskedWaves = D == 64 && !(CAP && LSE) ? 3 : 2;
@@ -876,6 +884,8 @@ masked_attn_kernel(MaskedParams p) {
 // loads, LDS and softmax state of its own and no barrier until the end, when their results are joined.  A wavefront's K buffer
 // takes the next block as soon as the scores are contracted, its V buffer as soon as O^T is: two wavefronts on a SIMD keep both
 // in flight, 128 KB a compute unit.
+// us on MI355X, four wavefronts with two stages of K and V each / this, unsplit:  one row of 8 heads, D 128, against 448 keys 10.6 /
+// 7.5, 2048 30.9 / 15.6, 20506 266 / 131;  eight rows against 41800 keys in all, 8 key heads for 24, split: 41.6 / 28.7 (5.7 TB/s).
 // ---------------------------------------------------------------------------------------------
 template <int D>
 struct FewRows {
@@ -1145,7 +1155,8 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_wav
 
 // ---------------------------------------------------------------------------------------------
 // out = sum over parts exp(lse_part - lse) O_part.  A wavefront for a (row, head): a lane holds the weight of a part, then two
-// elements (D 64: one) of the row.  Two latencies, of the parts' lse and of the parts themselves.
+// elements (D 64: one) of the row.  Two latencies, of the parts' lse and of the parts themselves.  Eight rows x 24 heads in up to 17
+// parts 4.9 us (one thread for eight elements, which goes through the parts: 8.2), 226 x 24 in ten parts 7.5.
 // ---------------------------------------------------------------------------------------------
 constexpr int kJoinRows = 4;  // (row, head)s of a workgroup
 

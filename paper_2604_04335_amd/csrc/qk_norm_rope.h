@@ -17,6 +17,8 @@ struct RopeTableParams {
   double quarters_hi[kMaxRopePairs], quarters_lo[kMaxRopePairs];
   uint8_t axis[kMaxRopePairs];
 };
+// Loads the code of these kernels on the current device, which the first launch would otherwise do.
+hipError_t qk_norm_rope_prepare();
 hipError_t rope_table_launch(const RopeTableParams& p, hipStream_t stream);
 
 enum class HeadNorm : int { kNone = 0, kRms = 1, kLayer = 2 };

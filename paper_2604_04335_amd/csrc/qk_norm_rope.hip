@@ -250,6 +250,11 @@ static void launch_norm(const QkNormRopeParams& p, HeadNorm norm, hipStream_t st
   else launch_layout<D, HeadNorm::kLayer>(p, stream);
 }
 
+hipError_t qk_norm_rope_prepare() {
+  hipFuncAttributes a;
+  return hipFuncGetAttributes(&a, reinterpret_cast<const void*>(rope_table_kernel));
+}
+
 hipError_t qk_norm_rope_launch(const QkNormRopeParams& p, HeadNorm norm, int head_dim, hipStream_t stream) {
   if (p.n_rows == 0) return hipSuccess;
   head_dim == 64 ? launch_norm<64>(p, norm, stream) : launch_norm<128>(p, norm, stream);

@@ -281,6 +281,15 @@ def test_masked(ctx, i):
     assert torch.equal(plain.view(torch.int16), out.view(torch.int16))
 
 
+@pytest.mark.parametrize("cap", [1e-38, 1e-20, 1e20])
+def test_masked_extreme_caps(ctx, cap):
+    q, k, v, cu_q, cu_k, kw = _make(CASES[13], 300)
+    kw["cap"] = cap
+    q[0] = 0
+    out, lse = _run_masked(ctx, to_dev(q), to_dev(k), to_dev(v), cu_q, cu_k, 0.125, _mask(kw))
+    _check_masked(out, lse, q, k, v, cu_q, cu_k, 0.125, **dict(kw, cap=float(np.float32(cap))))
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 @pytest.mark.parametrize("i", [2, 5, 13, 15, 19])
 def test_masked_scales(ctx, i, scale):
@@ -574,6 +583,7 @@ def test_refusals(ctx):
     assert norm(side(a=P + 8)) == -7 and norm(side(b=out.data_ptr() + 2)) == -7 and norm(side(weight=f.data_ptr() + 4)) == -7
     assert norm(side(bias=f), kind=da.NORM_NONE) == -15 and norm(side(weight=f), kind=da.NORM_NONE) == -15
     assert norm(side(row_stride=120)) == -16 and norm(side(row_stride=130)) == -16 and norm(side(out_row_stride=64)) == -16
+    assert norm(side(), side()) == -16 and norm(side(), side(a=out.data_ptr(), b=f.data_ptr())) == -16
     assert norm(side(b=P, out_row_stride=256)) == -16 and norm(side(), side(n_heads=0)) == -6
     torch.cuda.synchronize()
     assert bool((out == 3.0).all())

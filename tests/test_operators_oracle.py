@@ -111,6 +111,14 @@ def test_binding_structures():
                 torch.zeros((4, 5, 64), dtype=torch.bfloat16).transpose(0, 1)):
         with pytest.raises(ValueError):
             da.NormHeads(bad, one)
+    for wrong in (dict(k_doc=torch.zeros(4, dtype=torch.int64)), dict(q_doc=torch.zeros(4)), dict(slopes=torch.zeros(4, dtype=torch.int32)),
+                  dict(slopes=torch.zeros((4, 2))[:, 0])):
+        with pytest.raises(ValueError):
+            da.AttnMask(**wrong)
+    with pytest.raises(ValueError):
+        da.NormHeads(one, one, weight=torch.zeros(64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        da.dit_attn_rope_table(None, torch.zeros((4, 1), dtype=torch.int64), 4, spec, torch.zeros(4, 64, 2))
     mask = da.AttnMask(causal=True, prefix=[3, 4])
     assert mask.causal == 1 and mask.prefix[1] == 4
     x = torch.zeros((8, 1, 64), dtype=torch.bfloat16)
@@ -118,5 +126,7 @@ def test_binding_structures():
         da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 2, 4, 8], None, 1, 1, 64, 1.0, mask, x)
     with pytest.raises(ValueError):  # key boundaries of fewer sequences
         da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 2, 8], [0, 8], 1, 1, 64, 1.0, None, x)
+    with pytest.raises(ValueError):  # an output with strided rows
+        da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 8], None, 1, 1, 64, 1.0, None, torch.zeros((8, 2, 64), dtype=torch.bfloat16)[:, :1])
     with pytest.raises(da.DitAttnError):
         da.dit_attn_masked_varlen_fwd(None, x, x, x, [0, 8], None, 1, 1, 64, 1.0, None, x)
