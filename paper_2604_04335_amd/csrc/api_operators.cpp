@@ -208,6 +208,52 @@ int64_t choose_part_tiles(const std::vector<SeqWork>& seqs, bool few_rows, int32
   return tile_us * static_cast<double>(max_tiles - lo) > 4.0 + 0.33 * part_mb ? lo : max_tiles;
 }
 
+// Sequences of a call that one kernel takes, in launch order, and how their keys are split.
+struct MaskedBatch {
+  bool few_rows;
+  std::vector<int32_t> order;  // with query rows; the most keys first, once planned: their items take longest
+  std::vector<SeqWork> seqs;
+  int64_t part_tiles = 1, items = 0, tiles = 0, part_rows = 0;  // part_rows: of the partial results
+
+  size_t doc_bytes() const { return (static_cast<size_t>(tiles) * sizeof(dit::DocTile) + 255) / 256 * 256; }
+  size_t workspace_bytes(int32_t n_heads, int32_t head_dim, bool docs) const {
+    return (docs ? doc_bytes() : 0) +
+           static_cast<size_t>(part_rows) * static_cast<size_t>(n_heads) * (static_cast<size_t>(head_dim) + 1) * sizeof(float);
+  }
+};
+
+// Whether the sequences with few rows get a kernel of their own beside the others: where, as items of 128 rows, they would take
+// longer than its launch, by their work (0.65 us a tile and compute unit) or because their keys are the longest.  us, all as
+// items of 128 rows / in two kernels, D 128, 24 heads:  2 x 512 rows and 32 single rows against 4352 keys (8 key heads) 265 / 120, 4352
+// rows and one against 20506 keys 404 / 170;  D 64  4 x 1024 rows and 16 against 2000 keys (8) 55 / 43;  not worth one: 2 x 512 and
+// 4 against 1280 (8) 27 either way.
+bool worth_a_kernel(const MaskedBatch& few, const MaskedBatch& others, const int32_t* cu_k, int32_t n_heads, int n_cus) {
+  if (few.order.empty() || others.order.empty()) return true;
+  int64_t tiles = 0, longest = 0, longest_other = 0;
+  for (const int32_t i : few.order) {
+    tiles += tiles_of(cu_k[i + 1] - cu_k[i]);
+    longest = std::max(longest, tiles_of(cu_k[i + 1] - cu_k[i]));
+  }
+  for (const int32_t i : others.order) longest_other = std::max(longest_other, tiles_of(cu_k[i + 1] - cu_k[i]));
+  return 0.65 * static_cast<double>(tiles * n_heads) > 8.0 * n_cus || longest > longest_other + 16;
+}
+
+void plan_batch(MaskedBatch& b, const int32_t* cu_q, const int32_t* cu_k, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int n_cus) {
+  std::stable_sort(b.order.begin(), b.order.end(), [&](int32_t x, int32_t y) { return cu_k[x + 1] - cu_k[x] > cu_k[y + 1] - cu_k[y]; });
+  for (const int32_t i : b.order) {
+    const int64_t lq = cu_q[i + 1] - cu_q[i], tiles = tiles_of(cu_k[i + 1] - cu_k[i]);
+    b.seqs.push_back({b.few_rows ? n_kv_heads : (lq + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads, tiles, lq});
+    b.tiles += tiles;
+  }
+  if (b.seqs.empty()) return;
+  b.part_tiles = choose_part_tiles(b.seqs, b.few_rows, n_heads, head_dim, n_cus);
+  for (const SeqWork& w : b.seqs) {
+    const int64_t parts = parts_of(w.tiles, b.part_tiles);
+    b.items += w.items * parts;
+    if (parts > 1) b.part_rows += parts * w.rows;
+  }
+}
+
 int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* v, const int64_t* row_strides, const int32_t* cu_q,
                    const int32_t* cu_k, int32_t n_seqs, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
                    const dit_attn_mask* mask, void* out, float* lse, void* stream) {
@@ -243,53 +289,37 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   if (misaligned(lse, 4) || misaligned(m.slopes, 4) || misaligned(m.q_doc, 4) || misaligned(m.k_doc, 4))
     return fail(ctx, DIT_ATTN_ERR_ALIGN, "lse, slopes, q_doc and k_doc must be 4-byte aligned");
 
-  // Sequences with query rows, the most keys first: their items take longest.
-  std::vector<int32_t> order;
-  int64_t max_rows = 0, total_tiles = 0;
   const int32_t group = n_heads / n_kv_heads;
+  MaskedBatch batches[2];
+  batches[0].few_rows = true;
+  batches[1].few_rows = false;
   for (int32_t i = 0; i < n_seqs; ++i) {
-    const int64_t lq = cu_q[i + 1] - cu_q[i], tiles = tiles_of(cu_k[i + 1] - cu_k[i]);
-    if (lq == 0) continue;
-    order.push_back(i);
-    max_rows = std::max(max_rows, lq);
-    total_tiles += tiles;
-  }
-  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cu_k[a + 1] - cu_k[a] > cu_k[b + 1] - cu_k[b]; });
-  const bool few_rows = max_rows * group <= dit::kMaskedFewRows;
-  std::vector<SeqWork> seqs;
-  for (const int32_t i : order) {
     const int64_t lq = cu_q[i + 1] - cu_q[i];
-    seqs.push_back({few_rows ? n_kv_heads : (lq + dit::kMaskedBlockM - 1) / dit::kMaskedBlockM * n_heads, tiles_of(cu_k[i + 1] - cu_k[i]), lq});
+    if (lq > 0) batches[lq * group <= dit::kMaskedFewRows ? 0 : 1].order.push_back(i);
   }
-  dit::MaskedParams p{};
-  const int64_t part_tiles = choose_part_tiles(seqs, few_rows, n_heads, head_dim, ctx->n_cus);
-  p.part_tiles = static_cast<int32_t>(part_tiles);
-  int64_t items = 0, part_rows = 0;
-  for (size_t i = 0; i < order.size(); ++i) {
-    const int64_t parts = parts_of(seqs[i].tiles, part_tiles);
-    items += seqs[i].items * parts;
-    if (parts > 1) part_rows += parts * seqs[i].rows;
+  if (!worth_a_kernel(batches[0], batches[1], cu_k, n_heads, ctx->n_cus)) {
+    batches[1].order.insert(batches[1].order.end(), batches[0].order.begin(), batches[0].order.end());
+    std::sort(batches[1].order.begin(), batches[1].order.end());
+    batches[0].order.clear();
   }
-  if (items > 0x7FFFFFFF) return fail(ctx, DIT_ATTN_ERR_LIMIT, "pack has too many work items");
+  const bool docs = m.q_doc != nullptr;
+  size_t need = 0;
+  for (MaskedBatch& b : batches) {
+    plan_batch(b, cu_q, cu_k, n_heads, n_kv_heads, head_dim, ctx->n_cus);
+    if (b.items > 0x7FFFFFFF) return fail(ctx, DIT_ATTN_ERR_LIMIT, "pack has too many work items");
+    need = std::max(need, b.workspace_bytes(n_heads, head_dim, docs));
+  }
 
   dit::DeviceGuard guard;
   hipError_t e = guard.enter(ctx->device);
   if (e != hipSuccess) return fail_hip(ctx, e, "hipSetDevice");
   hipStream_t s = static_cast<hipStream_t>(stream);
 
-  const bool docs = m.q_doc != nullptr;
-  const size_t doc_bytes = docs ? (static_cast<size_t>(total_tiles) * sizeof(dit::DocTile) + 255) / 256 * 256 : 0;
-  const size_t part_rh = static_cast<size_t>(part_rows) * static_cast<size_t>(n_heads);
-  const size_t need = doc_bytes + part_rh * (static_cast<size_t>(head_dim) + 1) * sizeof(float);
-  if (need > 0) {
+  if (need > 0) {  // the second batch comes behind the first one on the stream and takes the same workspace
     rc = dit::ensure_workspace(ctx, need, dit::stream_capturing(s), "masked attention");
     if (rc != DIT_ATTN_OK) return rc;
-    if (docs) p.doc_tiles = reinterpret_cast<dit::DocTile*>(ctx->workspace);
-    if (part_rows > 0) {
-      p.part_out = ctx->workspace + doc_bytes / sizeof(float);
-      p.part_lse = p.part_out + part_rh * static_cast<size_t>(head_dim);
-    }
   }
+  dit::MaskedParams p{};
   p.q = q;
   p.k = k;
   p.v = v;
@@ -303,17 +333,18 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   if (m.softcap > 0.f) {
     // Finite, so that a score of 0 times it is 0.
     p.tanh_in = static_cast<float>(std::min(2.0 * 1.44269504088896340736 * std::fabs(static_cast<double>(scale)) / m.softcap, 3e38));
-    p.cap_log2 = m.softcap * 1.44269504088896340736f;
+    p.cap_log2 = static_cast<float>(std::min(m.softcap * 1.44269504088896340736, 3e38));
     // tanh(x) / x as a polynomial in x^2, off by at most 4e-7 relative for |x| <= 0.25 (a fit of least maximal error).
     const double a[3] = {0.9999996043443452, -0.33321908223103114, 0.12841613400294474};
     const double k = std::fabs(static_cast<double>(scale)) / m.softcap;
     // (Finite with scale 0, so that an infinite score is not among them, and with a finite square.)
     p.poly_up_to = static_cast<float>(std::min(0.25 / k, 1e18));
     // Exponents of at most 30 either way.
-    p.small = std::min(p.poly_up_to, static_cast<float>(30.0 / (1.44269504088896340736 * std::fabs(static_cast<double>(scale)))));
+    p.small = static_cast<float>(std::min<double>(p.poly_up_to, 30.0 / (1.44269504088896340736 * std::fabs(static_cast<double>(scale)))));
     for (int i = 0; i < 3; ++i) {
-      p.poly[i] = static_cast<float>(a[i] * m.softcap * 1.44269504088896340736 * std::pow(k, 2 * i + 1));
-      if (!std::isfinite(p.poly[i])) p.small = p.poly_up_to = -1.f;  // never
+      const double coefficient = a[i] * m.softcap * 1.44269504088896340736 * std::pow(k, 2 * i + 1);
+      if (std::fabs(coefficient) < 3e38) p.poly[i] = static_cast<float>(coefficient);
+      else p.small = p.poly_up_to = -1.f;  // never
     }
   }
   p.q_stride_b = 2 * strides[0];
@@ -323,40 +354,47 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   p.k_doc = m.k_doc;
   p.slopes = m.slopes;
   p.causal = m.causal;
-  const dit::MaskedKind kind = {head_dim, few_rows, m.softcap > 0.f, m.slopes != nullptr, lse != nullptr || part_rows > 0};
-  int64_t part_row = 0;
-  for (size_t first = 0; first < order.size(); first += dit::kMaskedSeqs) {
-    p.n = static_cast<int32_t>(std::min<size_t>(order.size() - first, dit::kMaskedSeqs));
-    uint32_t item = 0, tile = 0, join = 0;
-    int32_t n_join = 0;  // sequences with several parts come first: they have the most tiles
-    for (int32_t i = 0; i < p.n; ++i) {
-      const size_t at = first + static_cast<size_t>(i);
-      const int32_t sq = order[at];
-      const int64_t parts = parts_of(seqs[at].tiles, part_tiles);
-      dit::MaskedSeq& d = p.seq[i];
-      d.part_row = part_row;
-      d.first = item;
-      d.tile0 = tile;
-      d.join0 = join;
-      d.q_start = cu_q[sq];
-      d.q_len = cu_q[sq + 1] - cu_q[sq];
-      d.kv_start = cu_k[sq];
-      d.kv_len = cu_k[sq + 1] - cu_k[sq];
-      d.prefix = m.prefix ? m.prefix[sq] : 0;
-      d.parts = static_cast<int32_t>(parts);
-      item += static_cast<uint32_t>(seqs[at].items * parts);
-      tile += static_cast<uint32_t>(seqs[at].tiles);
-      if (parts > 1) {
-        part_row += parts * d.q_len;
-        join += dit::masked_join_blocks(d, n_heads);
-        ++n_join;
+  for (const MaskedBatch& b : batches) {
+    const size_t doc_bytes = docs ? b.doc_bytes() : 0;
+    p.part_tiles = static_cast<int32_t>(b.part_tiles);
+    p.doc_tiles = docs ? reinterpret_cast<dit::DocTile*>(ctx->workspace) : nullptr;
+    p.part_out = b.part_rows > 0 ? ctx->workspace + doc_bytes / sizeof(float) : nullptr;
+    p.part_lse = b.part_rows > 0 ? p.part_out + static_cast<size_t>(b.part_rows) * static_cast<size_t>(n_heads) * static_cast<size_t>(head_dim) : nullptr;
+    const dit::MaskedKind kind = {head_dim, b.few_rows, m.softcap > 0.f, m.slopes != nullptr, lse != nullptr || b.part_rows > 0};
+    int64_t part_row = 0;
+    for (size_t first = 0; first < b.order.size(); first += dit::kMaskedSeqs) {
+      p.n = static_cast<int32_t>(std::min<size_t>(b.order.size() - first, dit::kMaskedSeqs));
+      uint32_t item = 0, tile = 0, join = 0;
+      int32_t n_join = 0;  // sequences with several parts come first: they have the most tiles
+      for (int32_t i = 0; i < p.n; ++i) {
+        const size_t at = first + static_cast<size_t>(i);
+        const int32_t sq = b.order[at];
+        const int64_t parts = parts_of(b.seqs[at].tiles, b.part_tiles);
+        dit::MaskedSeq& d = p.seq[i];
+        d.part_row = part_row;
+        d.first = item;
+        d.tile0 = tile;
+        d.join0 = join;
+        d.q_start = cu_q[sq];
+        d.q_len = cu_q[sq + 1] - cu_q[sq];
+        d.kv_start = cu_k[sq];
+        d.kv_len = cu_k[sq + 1] - cu_k[sq];
+        d.prefix = m.prefix ? m.prefix[sq] : 0;
+        d.parts = static_cast<int32_t>(parts);
+        item += static_cast<uint32_t>(b.seqs[at].items * parts);
+        tile += static_cast<uint32_t>(b.seqs[at].tiles);
+        if (parts > 1) {
+          part_row += parts * d.q_len;
+          join += dit::masked_join_blocks(d, n_heads);
+          ++n_join;
+        }
       }
+      p.n_items = item;
+      e = dit::masked_attn_launch(p, kind, docs ? tile : 0, s);
+      if (e != hipSuccess) return fail_hip(ctx, e, "masked attention kernel launch");
+      e = dit::masked_join_launch(p, n_join, join, head_dim, s);
+      if (e != hipSuccess) return fail_hip(ctx, e, "join kernel launch");
     }
-    p.n_items = item;
-    e = dit::masked_attn_launch(p, kind, docs ? tile : 0, s);
-    if (e != hipSuccess) return fail_hip(ctx, e, "masked attention kernel launch");
-    e = dit::masked_join_launch(p, n_join, join, head_dim, s);
-    if (e != hipSuccess) return fail_hip(ctx, e, "join kernel launch");
   }
   return DIT_ATTN_OK;
 }

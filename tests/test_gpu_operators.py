@@ -243,6 +243,10 @@ CASES = [
     ([40], [2500], 1, 1, 128, dict()),
     ([1000], None, 8, 8, 128, dict(causal=True)),
     ([1100], None, 8, 2, 64, dict(bias=True)),
+    # few rows and others in one pack: two kernels, both of which split their keys, and one kernel
+    ([1, 300, 2, 0, 40], [3000, 300, 5000, 10, 1500], 2, 1, 128, dict(causal=True, docs=2, pad=20, prefix=[0, 40, 10, 0, 9])),
+    ([3, 1, 500], [900, 4000, 2500], 3, 1, 64, dict(cap=20.0, bias=True)),
+    ([20, 200], [20, 200], 2, 2, 128, dict(causal=True)),
 ]
 
 
