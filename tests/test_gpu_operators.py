@@ -155,6 +155,34 @@ def test_norm_rope(ctx, n, H, G, D, norm, half, rot, affine, fused):
     assert np.array_equal(to_bits(qkv[:, (H + G) * D:]), bits[:, (H + G) * D:])
 
 
+@pytest.mark.parametrize("D,rot,half,norm", [(128, 128, True, da.NORM_RMS), (128, 40, True, da.NORM_LAYER), (64, 64, False, da.NORM_RMS),
+                                             (64, 48, True, da.NORM_NONE)])
+@pytest.mark.parametrize("rows", [7001, 30011])
+def test_large_calls_give_the_bits_of_small_ones(ctx, rows, D, rot, half, norm):
+    """Sizes with streaming loads (over 64 MB) and with streaming stores too (over 160 MB), out of place and in place."""
+    H, G = (24, 8) if D == 128 else (48, 16)
+    gen = torch.Generator(device="cuda").manual_seed(rows + rot)
+    q, k = (torch.randn((rows, h, D), device="cuda", generator=gen).to(torch.bfloat16) for h in (H, G))
+    angle = torch.randn((rows, rot // 2), device="cuda", generator=gen) * 100
+    table = torch.stack([angle.cos(), angle.sin()], 2)
+    w = torch.randn(D, device="cuda", generator=gen) if norm != da.NORM_NONE else None
+    layout = da.ROPE_HALF if half else da.ROPE_INTERLEAVED
+
+    def call(a, b, qo, ko):
+        da.dit_attn_qk_norm_rope(ctx, da.NormHeads(q[a:b], qo[a:b], w, w), da.NormHeads(k[a:b], ko[a:b], w, w), b - a, D, norm, 1e-6,
+                                 table[a:b], rot, layout, _stream())
+
+    small, large = [[torch.empty_like(q), torch.empty_like(k)] for _ in range(2)]
+    for a in range(0, rows, 1000):
+        call(a, min(rows, a + 1000), *small)
+    call(0, rows, *large)
+    for x, y in zip(small, large):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+    call(0, rows, q, k)
+    for x, y in zip(small, (q, k)):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
 def test_norm_of_zeros_and_of_rows_with_infinities(ctx):
     """A row of zeros stays zero (with eps), and rows that are not finite do not reach the others."""
     x = torch.ones((64, 2, 128), dtype=torch.bfloat16, device="cuda")
