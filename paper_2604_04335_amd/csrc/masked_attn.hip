@@ -485,6 +485,10 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
   SCHED_FENCE();
 }
 
+// Workgroups on a compute unit: what the registers allow.
+template <int D, bool CAP, bool LSE>
+constexpr int kMaskedWaves = D == 64 && !(CAP && LSE) ? 3 : 2;
+
 // The kernel works a tile ahead, as the unmasked 128-row kernel: the scores of the next tile are contracted beside the softmax of
 // this one.  Most tiles are touched by no mask; runs of them have a loop of their own, in which a cap and a bias cost their few
 // instructions a score beside the MFMAs.  What else shapes and masks a tile's scores stands between two steps.
@@ -493,10 +497,6 @@ __device__ __forceinline__ void masked_step(const int (&va_)[T::NDB], const int 
 // bias 987 / 769, padded documents of three 559 / 412.  Bound by power (1.7 GHz) with both pipes of a SIMD over half busy; the
 // padded documents by vector instructions, half of their tiles being at an edge of a document or around the rows' own places.
 // 128 rows and not 64 or 256: two workgroups of four wavefronts fill a compute unit's registers and 130 of its 160 KB LDS.
-// Workgroups on a compute unit: what the registers allow.
-template <int D, bool CAP, bool LSE>
-constexpr int kMaskedWaves = D == 64 && !(CAP && LSE) ? 3 : 2;
-
 template <class T, bool CAP, bool BIAS, bool LSE>
 __global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu_waves_per_eu(kMaskedWaves<T::D, CAP, LSE>, kMaskedWaves<T::D, CAP, LSE>)))
 masked_attn_kernel(MaskedParams p) {
@@ -525,6 +525,7 @@ masked_attn_kernel(MaskedParams p) {
   local /= (uint32_t)sq.parts;
   it.head = (int)(local % (uint32_t)n_heads);
   const int m0 = ((lq + T::BM - 1) / T::BM - 1 - (int)(local / (uint32_t)n_heads)) * T::BM;
+  static_assert(T::BM == kMaskedBlockM, "items as the host counts them");
   it.q_start = sq.q_start + m0;
   it.q_rows = lq - m0 < T::BM ? lq - m0 : T::BM;
   it.kv_start = sq.kv_start;
