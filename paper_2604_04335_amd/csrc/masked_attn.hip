@@ -257,27 +257,33 @@ __device__ __forceinline__ uint32_t make_finite(uint32_t addr, uint32_t step) {
   return found;
 }
 
-// Behind the loop of an item some of whose rows see a value that is not finite in a masked tile: such values of keys
-// [key0, key1), key stride `step` in blocks of `run`, are added to the rows that see them.  Slow, and seldom.
+// Behind the loop of an item some of whose rows (poison: this lane's) see a value that is not finite in a masked tile: such values
+// of keys [key0, key1), key stride `step` in blocks of `run`, are added to the rows that see them, until nothing can change any
+// more.  Slow, and seldom: about a microsecond a key.
 template <class T>
 __device__ __forceinline__ void add_not_finite(const MaskedParams& p, const char* vbase, const int32_t* kdoc, int key0, int key1, int run,
-                                               int step, int klim, int doc, int hh, f32x16 (&o)[T::NDB]) {
+                                               int step, int klim, int doc, int hh, bool poison, f32x16 (&o)[T::NDB]) {
   for (int b = key0; b < key1; b += step)
     for (int j = b; j < b + run && j < key1; ++j) {
       const uint32_t* row = reinterpret_cast<const uint32_t*>(vbase + (int64_t)j * p.v_stride_b);
-      const int lane = threadIdx.x & 63;
-      const bool bad = pair_not_finite(row[lane & (T::D / 2 - 1)]);
-      if (__builtin_amdgcn_ballot_w64(bad) == 0) continue;
+      const uint32_t w = row[threadIdx.x & (T::D / 2 - 1)];  // a pair of elements in each of the first D / 2 lanes
+      const uint64_t pairs = __builtin_amdgcn_ballot_w64(pair_not_finite(w));
+      if (pairs == 0) continue;
       const bool seen = j < klim && (kdoc == nullptr || kdoc[j] == doc);
+      bool all_nan = true;
 #pragma unroll
       for (int db = 0; db < T::NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int d = 32 * db + 8 * (i >> 2) + (i & 3) + 4 * hh;
-          const uint32_t w = row[d >> 1], bits = d & 1 ? w & 0xFFFF0000u : w << 16;
-          if (seen && (bits & 0x7F800000u) == 0x7F800000u) o[db][i] += __builtin_bit_cast(float, bits);
-          asm volatile("" : "+v"(o[db][i])::"memory");  // one at a time: this may not cost the tile loop registers
+          const int d = 32 * db + 8 * (i >> 2) + (i & 3);  // and 4 more in the upper half of the wavefront
+          const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)w, d >> 1), hi = (uint32_t)__builtin_amdgcn_readlane((int)w, (d >> 1) + 2);
+          const uint32_t x = hh ? hi : lo, bits = d & 1 ? x & 0xFFFF0000u : x << 16;
+          const float sum = o[db][i] + __builtin_bit_cast(float, bits);
+          o[db][i] = seen && (bits & 0x7F800000u) == 0x7F800000u ? sum : o[db][i];
+          all_nan &= o[db][i] != o[db][i];
+          asm volatile("" : "+v"(o[db][i]));  // one at a time: this may not cost the tile loop registers
         }
+      if (__builtin_amdgcn_ballot_w64(poison && !all_nan) == 0) key1 = key0;
     }
 }
 
@@ -859,7 +865,7 @@ masked_attn_kernel(MaskedParams p) {
       const int k0 = it.part * p.part_tiles * T::BN;
       int doc;
       const int klim = row_mask(query_row(), doc);
-      add_not_finite<T>(p, vbase, kdoc, k0, tiles.end * T::BN < lim ? tiles.end * T::BN : lim, T::BN, T::BN, klim, doc, half_of(tid), o);
+      add_not_finite<T>(p, vbase, kdoc, k0, tiles.end * T::BN < lim ? tiles.end * T::BN : lim, T::BN, T::BN, klim, doc, half_of(tid), poison, o);
     }
     // The rows are staged in the K buffers, which nobody reads behind the last barrier.
   }
@@ -1093,7 +1099,7 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_wav
     if (__builtin_amdgcn_ballot_w64(poison) != 0) {
       int doc;
       const int klim = row_mask(doc);
-      add_not_finite<T>(p, vbase, kdoc, first_block * F::KEYS, n_blocks * F::KEYS < lim ? n_blocks * F::KEYS : lim, F::KEYS, F::KEYS * F::WAVES, klim, doc, hh, o);
+      add_not_finite<T>(p, vbase, kdoc, first_block * F::KEYS, n_blocks * F::KEYS < lim ? n_blocks * F::KEYS : lim, F::KEYS, F::KEYS * F::WAVES, klim, doc, hh, poison, o);
     }
   }
 

@@ -383,6 +383,24 @@ def test_what_a_row_does_not_see_has_no_effect(ctx, few, D, parts):
     assert torch.equal(lse[:r[2]], clean_lse[:r[2]]) and torch.equal(lse[:, 0], clean_lse[:, 0])
 
 
+@pytest.mark.parametrize("rows", [2, 700])
+def test_values_that_are_nowhere_finite(ctx, rows):
+    """All values NaN, or one element of each infinite: every row that sees a key gets them, and the call ends soon."""
+    rng = _rng(rows)
+    n, H, D = 3000, 4, 128
+    q, k, v = to_dev(_bf16(rng, rows, H, D)), to_dev(_bf16(rng, n, H, D)), to_dev(_bf16(rng, n, H, D))
+    mask = da.AttnMask(causal=True)
+    clean, _ = _run_masked(ctx, q, k, v, _cu([rows]), _cu([n]), 0.1, mask)
+    v[:, :, 77] = float("inf")
+    out, _ = _run_masked(ctx, q, k, v, _cu([rows]), _cu([n]), 0.1, mask)
+    assert bool(torch.isinf(out[:, :, 77]).all())
+    keep = [d for d in range(D) if d != 77]
+    assert torch.equal(out[:, :, keep].view(torch.int16), clean[:, :, keep].view(torch.int16))
+    v.fill_(float("nan"))
+    out, _ = _run_masked(ctx, q, k, v, _cu([rows]), _cu([n]), 0.1, mask)
+    assert bool(torch.isnan(out).all())
+
+
 @pytest.mark.parametrize("lq,lk,D", [(400, 400, 64), (200, 400, 128), (6, 700, 64), (6, 700, 128), (140, 3000, 128)])
 def test_padding_and_other_documents_may_hold_anything(ctx, lq, lk, D):
     rng = _rng(lq + D)
