@@ -181,6 +181,9 @@ __device__ __forceinline__ bool sees(const f32x16 (&s)[NKB], uint64_t keys, int 
   return any;
 }
 
+// Whether either lane of a row says so: they hold the scores of different keys, and other elements of the result.
+__device__ __forceinline__ bool either_half(bool x) { return x | (__shfl_xor((int)x, 32) != 0); }
+
 // Which half of its wavefront a lane is in; recomputed where it is needed.
 __device__ __forceinline__ int half_of(int tid) {
   asm volatile("" : "+v"(tid));
@@ -257,9 +260,9 @@ __device__ __forceinline__ uint32_t make_finite(uint32_t addr, uint32_t step) {
   return found;
 }
 
-// Behind the loop of an item some of whose rows (poison: this lane's) see a value that is not finite in a masked tile: such values
-// of keys [key0, key1), key stride `step` in blocks of `run`, are added to the rows that see them, until nothing can change any
-// more.  Slow, and seldom: about a microsecond a key.
+// Behind the loop of an item some of whose rows (poison: this lane's row, in both of its lanes) see a value that is not finite in
+// a masked tile: such values of keys [key0, key1), key stride `step` in blocks of `run`, are added to the rows that see them, until
+// nothing can change any more.  Slow, and seldom: about a microsecond a key.
 template <class T>
 __device__ __forceinline__ void add_not_finite(const MaskedParams& p, const char* vbase, const int32_t* kdoc, int key0, int key1, int run,
                                                int step, int klim, int doc, int hh, bool poison, f32x16 (&o)[T::NDB]) {
@@ -861,6 +864,7 @@ masked_attn_kernel(MaskedParams p) {
     masked_softmax<T::NKB, T::NDB, LSE>(sa, mx, c, pb, o, r);
     mfma_stream<T, true, 0, 0, kPrefetch>(smem, va, ka, pb, qf, o, sa);
     r.l += row_sum<T>(pb);
+    poison = either_half(poison);
     if (__builtin_amdgcn_ballot_w64(poison) != 0) {
       const int k0 = it.part * p.part_tiles * T::BN;
       int doc;
@@ -1096,6 +1100,7 @@ __global__ void __attribute__((amdgpu_flat_work_group_size(512, 512), amdgpu_wav
       block = next;
       turn ^= 1;
     }
+    poison = either_half(poison);
     if (__builtin_amdgcn_ballot_w64(poison) != 0) {
       int doc;
       const int klim = row_mask(doc);
