@@ -170,6 +170,10 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[NKB], LaneMask m, bool h
       }
 }
 
+// A mask of 64 keys from its words, which readfirstlane returns as signed numbers: key 31 is not the sign of the others.
+__host__ __device__ constexpr uint64_t mask_of_words(int lo, int hi) { return (uint64_t)(uint32_t)lo | (uint64_t)(uint32_t)hi << 32; }
+static_assert(mask_of_words(INT32_MIN, 0) == 1ull << 31 && mask_of_words(-1, INT32_MIN) == 0x80000000FFFFFFFFull, "no sign extension");
+
 // Whether this lane's row sees one of the keys whose bits are set.
 template <int NKB>
 __device__ __forceinline__ bool sees(const f32x16 (&s)[NKB], uint64_t keys, int hh) {
@@ -706,8 +710,8 @@ masked_attn_kernel(MaskedParams p) {
     auto look_bad = [&](const f32x16(&s)[T::NKB], bool masked) {
       if (masked) {
         const uint32_t at = lds + kBadOff<T> + (uint32_t)turn * 8u;
-        const uint64_t bad = (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)at) |
-                             (uint64_t)__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)(at + 4)) << 32;
+        const uint64_t bad = mask_of_words(__builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)at),
+                                           __builtin_amdgcn_readfirstlane(*(lds_u32*)(uintptr_t)(at + 4)));
         if (bad != 0) poison |= sees<T::NKB>(s, bad, half_of(tid));
       }
       const int clear = turn == 0 ? 2 : turn - 1;

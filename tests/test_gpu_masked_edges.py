@@ -1,4 +1,4 @@
-"""GPU tests of masked attention where it can go wrong: values that are not finite among the keys that a row sees."""
+"""GPU tests of masked attention where it can go wrong: values that are not finite among seen and unseen keys."""
 import os
 import sys
 
@@ -38,3 +38,34 @@ def test_values_of_two_keys_that_are_nan_in_turn(ctx, D, few, first):
     assert 0 < a - pos0 < lq - 2
     assert torch.equal(torch.isnan(out), want)
     assert torch.equal(out[~want].view(torch.int16), clean[~want].view(torch.int16)) and torch.equal(lse, clean_lse)
+
+
+def test_an_unseen_value_costs_nothing(ctx):
+    """A key of another document whose value is NaN, at every place of a tile: the call takes as long as for any other place, not a
+    walk over all keys."""
+    rng = _rng(4)
+    lq, lk, H, D = 128, 8192, 64, 64
+    q, k, v = to_dev(_bf16(rng, lq, H, D)), to_dev(_bf16(rng, lk, H, D)), to_dev(_bf16(rng, lk, H, D))
+    out = torch.empty_like(q)
+    q_doc = torch.zeros(lq, dtype=torch.int32, device="cuda")
+
+    def time_of(place):
+        ids = torch.zeros(lk, dtype=torch.int32, device="cuda")
+        ids[place::64] = 1
+        values = v.clone()
+        values[place::64] = float("nan")
+        mask = da.AttnMask(q_doc=q_doc, k_doc=ids)
+        best = float("inf")
+        for _ in range(4):
+            start, end = torch.cuda.Event(True), torch.cuda.Event(True)
+            start.record()
+            da.dit_attn_masked_varlen_fwd(ctx, q, k, values, _cu([lq]), _cu([lk]), H, H, D, 0.125, mask, out)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        assert bool(torch.isfinite(out.float()).all())
+        return best
+
+    usual = time_of(30)
+    for place in (0, 31, 32, 63):
+        assert time_of(place) < 3 * usual, place
