@@ -1,7 +1,9 @@
-"""GPU tests of masked attention where it can go wrong: values that are not finite among seen and unseen keys."""
+"""GPU tests of masked attention where it can go wrong: values that are not finite among seen and unseen keys, and a distance bias
+in runs of whole tiles, with and without document ids."""
 import os
 import sys
 
+import numpy as np
 import pytest
 import torch
 
@@ -9,7 +11,7 @@ import paper_2604_04335_amd as da
 
 sys.path.insert(0, os.path.dirname(__file__))
 from gpu_util import to_dev  # noqa: E402
-from test_gpu_operators import _bf16, _cu, _rng, _run_masked, ctx  # noqa: E402, F401
+from test_gpu_operators import _bf16, _check_masked, _cu, _make, _mask, _rng, _run_masked, ctx  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +71,30 @@ def test_an_unseen_value_costs_nothing(ctx):
     usual = time_of(30)
     for place in (0, 31, 32, 63):
         assert time_of(place) < 3 * usual, place
+
+
+BIAS_CASES = [
+    # q lens, k lens (None: the same), H, G, D, options: runs that begin and end at documents, behind the rows and before them
+    ([1500], None, 2, 2, 64, dict(bias=True, docs=2, pad=101)),
+    ([1500], None, 2, 1, 128, dict(bias=True, docs=2, pad=101)),
+    ([1500], None, 2, 2, 128, dict(bias=True, docs=2, pad=0, causal=True)),
+    ([1500], None, 2, 2, 64, dict(bias=True, docs=2, pad=64, causal=True, prefix=[700])),
+    ([1300], None, 2, 2, 128, dict(bias=True)),                        # over 600 keys behind the first rows
+    ([200, 900], [1200, 900], 2, 2, 128, dict(bias=True, docs=1, pad=5)),
+    ([700, 130], [700, 2000], 2, 1, 64, dict(bias=True, docs=3, pad=0, shuffle=True)),
+    ([3], [900], 4, 2, 128, dict(bias=True, docs=3, pad=50)),
+    ([9], [2100], 2, 1, 64, dict(bias=True, docs=2, pad=0, causal=True)),
+]
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("i", range(len(BIAS_CASES)))
+def test_bias_with_and_without_documents(ctx, i, sign):
+    print(BIAS_CASES[i], flush=True)
+    q, k, v, cu_q, cu_k, kw = _make(BIAS_CASES[i], 400 + i)
+    kw["slopes"] = (sign * kw["slopes"]).astype(np.float32)
+    scale = q.shape[2] ** -0.5
+    out, lse = _run_masked(ctx, to_dev(q), to_dev(k), to_dev(v), cu_q, cu_k, scale, _mask(kw))
+    _check_masked(out, lse, q, k, v, cu_q, cu_k, scale, **kw)
+    plain, _ = _run_masked(ctx, to_dev(q), to_dev(k), to_dev(v), cu_q, cu_k, scale, _mask(kw), want_lse=False)
+    assert torch.equal(plain.view(torch.int16), out.view(torch.int16))
