@@ -388,7 +388,7 @@ enum class Shape : int {
   kNone,
   kCap,     // sc are raw scores; their exponent is sc * (poly[0] + poly[1] sc^2 + poly[2] sc^4) - mc, see shape_scores
   kLinear,  // a bias that is linear over the tile: the accumulators of S^T(t+1) hold slope * key + start already, and those of
-            // S^T(t), once their exponentials are taken, get what S^T(t+2) begins with
+            // S^T(t), once their exponentials are taken, get what S^T(t+2) begins with (relative to the run's largest bias)
 };
 
 // One step: the exponentials of tile t beside the MFMAs of S^T(t+1) = K(t+1) Q^T and of O^T += V(t)^T P(t)^T, in the slots of
@@ -750,8 +750,13 @@ masked_attn_kernel(MaskedParams p) {
     const char *kp = kbase, *vp = vbase;
     const int64_t k_step = (int64_t)T::BN * p.k_stride_b, v_step = (int64_t)T::BN * p.v_stride_b;
     constexpr Shape SHAPE = BIAS ? (CAP ? Shape::kNone : Shape::kLinear) : CAP ? Shape::kCap : Shape::kNone;
-    // With kLinear all keys of a run lie on one side of all rows, and its bias is side * (key - pos).
+    // With kLinear all keys of a run lie on one side of all rows, and its bias is side * (key - pos).  An accumulator that began
+    // with that would round every product at the size of the bias, so within a run scores and their reference are relative to
+    // the row's largest bias there, of key `anchor`: those that count then are small.
     float side = 0.f;
+    int anchor = 0;
+    auto anchor_bias = [&]() { return side * (float)(anchor - pos0 - query_row()); };
+    auto linear_start = [&](int t) { return side * (float)(t * T::BN + 4 * half_of(tid) - anchor); };
     // A step from t (scores raw with kCap, else shaped, in sc; K(t + 1) and V(t) on their way) to t + 1 (in sn, shaped with
     // kLinear, else raw).
     auto run_step = [&](auto uc, f32x16(&sc)[T::NKB], f32x16(&sn)[T::NKB]) {
@@ -770,7 +775,7 @@ masked_attn_kernel(MaskedParams p) {
           mx = tile_max<T>(sc);
         }
       }
-      const float start = SHAPE == Shape::kLinear ? -side * (float)distance(t0 + 2) : 0.f;
+      const float start = SHAPE == Shape::kLinear ? linear_start(t0 + 2) : 0.f;
       raise();
       const float mc = __builtin_fmaxf(r.m_ref * c, -3.0e38f);
       masked_step<T, (1 - U) * T::TILE_B, U * T::TILE_B, T::D == 64 && SHAPE == Shape::kLinear ? 3 : kPrefetch, SHAPE, CAP, LSE>(
@@ -819,8 +824,14 @@ masked_attn_kernel(MaskedParams p) {
           kp = kbase + (int64_t)(t0 + 2) * k_step;
           vp = vbase + (int64_t)(t0 + 1) * v_step;
           if constexpr (SHAPE == Shape::kLinear) {
-            finish(sa, t0, 0, false);
-            linear_scores<T::NKB>(sb, side, -side * (float)distance(t0 + 1));
+            anchor = side > 0.f ? run_end * T::BN - 1 : t0 * T::BN;
+            r.m_ref -= anchor_bias();
+            linear_scores<T::NKB>(sb, side, linear_start(t0));
+#pragma unroll
+            for (int kb = 0; kb < T::NKB; ++kb) sa[kb] += sb[kb];
+            scores_ready<T>(sa);
+            mx = tile_max<T>(sa);
+            linear_scores<T::NKB>(sb, side, linear_start(t0 + 1));
           }
           do {
             if constexpr (SHAPE == Shape::kNone && BIAS) finish(sa, t0, 0, false);
@@ -828,7 +839,16 @@ masked_attn_kernel(MaskedParams p) {
             if constexpr (SHAPE == Shape::kNone && BIAS) finish(sb, t0, 0, false);
             run_step(IC<1>{}, sb, sa);
           } while (t0 + 3 < run_end);
-          shaped = SHAPE == Shape::kLinear;
+          if constexpr (SHAPE == Shape::kLinear) {
+            const float base = anchor_bias();
+            r.m_ref += base;
+            mx += base;
+#pragma unroll
+            for (int kb = 0; kb < T::NKB; ++kb)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) sa[kb][i] += base;
+            shaped = true;
+          }
           t1 = t0 + 1;
           t2 = tiles.next(t1 + 1);
           masked0 = masked1 = false;

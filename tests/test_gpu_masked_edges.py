@@ -98,3 +98,46 @@ def test_bias_with_and_without_documents(ctx, i, sign):
     _check_masked(out, lse, q, k, v, cu_q, cu_k, scale, **kw)
     plain, _ = _run_masked(ctx, to_dev(q), to_dev(k), to_dev(v), cu_q, cu_k, scale, _mask(kw), want_lse=False)
     assert torch.equal(plain.view(torch.int16), out.view(torch.int16))
+
+
+@pytest.mark.parametrize("where", ["left", "right"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_bias_where_the_keys_that_count_lie_far_away(ctx, D, where):
+    """Keys that count at a distance of 2^19 and a bias there of 2^18: fp32 has steps of 2^-5 at that size, so a sum of products
+    that begins with the bias is off by several per cent of a probability.  Relative to the largest bias of the row the scores
+    that count are small, and the result is as near as without a bias.  In whole tiles, where no mask is looked at.
+      left   rows at the end, a slope of -1/2 (the farthest keys count: the first ones)
+      right  rows at the beginning of as many (without a document: they see nothing), keys of the rows' document far behind them"""
+    rng = _rng(D)
+    far, near, H = 2 ** 19, 4096, 1
+    slope = 0.5
+    scale = D ** -0.5
+    live = 128  # a whole item: no row of it without a document
+    if where == "left":
+        lq, lk, sign, keys = live, far, -1.0, slice(0, near)
+        ids = {}
+    else:
+        lq = lk = far + near
+        sign, keys = 1.0, slice(far, far + near)
+        q_doc, k_doc = torch.full((lq,), -1, dtype=torch.int32, device="cuda"), torch.full((lk,), -1, dtype=torch.int32, device="cuda")
+        q_doc[:live] = 0
+        k_doc[keys] = 0
+        ids = dict(q_doc=q_doc, k_doc=k_doc)
+    q, k, v = (torch.randn((n, H, D), device="cuda", generator=torch.Generator("cuda").manual_seed(D + n_)).to(torch.bfloat16)
+               for n_, n in enumerate((lq, lk, lk)))
+    slopes = torch.full((H,), sign * slope, device="cuda")
+    out, lse = _run_masked(ctx, q, k, v, _cu([lq]), _cu([lk]), scale, da.AttnMask(slopes=slopes, **ids))
+    # the keys that count, in 64 bits; others are under 2^-1000 of them
+    kk, vv, qq = (x.double().cpu().numpy() for x in (k[keys, 0], v[keys, 0], q[:live, 0]))
+    dist = np.abs(np.arange(live)[:, None] + (lk - lq) - np.arange(lk)[keys][None, :])
+    s = qq @ kk.T * scale - sign * slope * dist
+    m = s.max(1, keepdims=True)
+    p = np.exp(s - m)
+    want, spread = p @ vv / p.sum(1, keepdims=True), p @ np.abs(vv) / p.sum(1, keepdims=True)
+    # half a step of the result; the probabilities' rounding and, a tenth of it, fp32 scores of up to 64
+    bound = 2.0 ** -8 * np.abs(want) + 1.1 * 2.0 ** -8 * (spread + np.abs(want))
+    got = out[:live, 0].double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= bound), float(np.max(np.abs(got - want) / bound))
+    # the bias, the reference taken off and put on again, two products and the result: half a step of the largest each
+    want_lse = m[:, 0] + np.log(p.sum(1))
+    assert np.all(np.abs(lse[:live, 0].double().cpu().numpy() - want_lse) <= 8 * 2.0 ** -24 * np.abs(m[:, 0]) + 1e-5)
