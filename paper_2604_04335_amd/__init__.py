@@ -12,7 +12,9 @@ There is no CPU fallback: if the shared library has not been built
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+import struct
 
 import numpy as np
 
@@ -131,12 +133,65 @@ class NormHeads(ctypes.Structure):
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("n_heads", ctypes.c_int32)]
 
     def __init__(self, x, out, weight=None, bias=None, n_heads=None, row_stride=None, out_row_stride=None):
-        if n_heads is None:
-            n_heads = x.shape[1]
-        super().__init__(_ptr(x), _ptr(out), _row_stride(x, "x") if row_stride is None else int(row_stride),
-                         _row_stride(out, "out") if out_row_stride is None else int(out_row_stride), _array(weight, "weight", True),
-                         _array(bias, "bias", True), int(n_heads))
+        # What a call has to agree with: the shapes of tensors whose strides are their own, the elements of weight and bias, and the
+        # device of all (of which -2 is none).
+        x_shape = out_shape = device = n_weight = None
+        if hasattr(x, "stride"):
+            x_shape, device, self.x = x.shape, x.get_device(), x.data_ptr()
+            if n_heads is None:
+                n_heads = x_shape[1]
+            if row_stride is None:
+                row_stride = _row_stride(x, "x", x_shape)
+            else:
+                _check_kind(x, "x", _BF16)
+                x_shape = None
+        else:
+            self.x = _ptr(x)
+        if hasattr(out, "stride"):
+            out_shape, where, self.out = out.shape, out.get_device(), out.data_ptr()
+            if out_row_stride is None:
+                out_row_stride = _row_stride(out, "out", out_shape)
+                if out_shape == x_shape:
+                    out_shape = None
+            else:
+                _check_kind(out, "out", _BF16)
+                out_shape = None
+            if where != device:
+                device = where if device is None else -2
+        else:
+            self.out = _ptr(out)
+        # (Fields are 0 to begin with.)
+        if row_stride:
+            self.row_stride = int(row_stride)
+        if out_row_stride:
+            self.out_row_stride = int(out_row_stride)
+        self.n_heads = int(n_heads)
+        if weight is not None:
+            self.weight = _array(weight, "weight", _FP32)
+            if hasattr(weight, "stride"):
+                n_weight, where = weight.numel(), weight.get_device()
+                if where != device:
+                    device = where if device is None else -2
+        if bias is not None:
+            self.bias = _array(bias, "bias", _FP32)
+            if hasattr(bias, "stride"):
+                n, where = bias.numel(), bias.get_device()
+                n_weight = n if n_weight is None or n < n_weight else n_weight
+                if where != device:
+                    device = where if device is None else -2
         self._held = (x, out, weight, bias)
+        self._needs = (x_shape, out_shape, n_weight, device)
+
+    def _check(self, n_rows: int, head_dim: int, on) -> None:
+        x_shape, out_shape, n_weight, device = self._needs
+        if x_shape is not None:
+            _check_size("x", x_shape, n_rows, self.n_heads, head_dim)
+        if out_shape is not None:
+            _check_size("out", out_shape, n_rows, self.n_heads, head_dim)
+        if n_weight is not None and n_weight < head_dim:
+            raise ValueError(f"weight, bias: at least {head_dim} elements, not {n_weight}")
+        if device != on and device is not None:
+            _check_device("x, out, weight, bias", device, on)
 
 
 class AttnMask(ctypes.Structure):
@@ -151,8 +206,8 @@ class AttnMask(ctypes.Structure):
             prefix = [int(x) for x in prefix]
             self.n_prefix = len(prefix)
             prefix = (ctypes.c_int32 * max(len(prefix), 1))(*prefix)
-        super().__init__(int(causal), float(softcap), prefix, _array(slopes, "slopes", True), _array(q_doc, "q_doc", False),
-                         _array(k_doc, "k_doc", False))
+        super().__init__(int(causal), float(softcap), prefix, _array(slopes, "slopes", _FP32), _array(q_doc, "q_doc", _INT32),
+                         _array(k_doc, "k_doc", _INT32))
         self._held = (prefix, slopes, q_doc, k_doc)
 
 
@@ -229,6 +284,8 @@ def load_library() -> ctypes.CDLL:
 
 
 def _ptr(x) -> int:
+    if type(x) is int:
+        return x
     if x is None:
         return 0
     if hasattr(x, "data_ptr"):
@@ -238,26 +295,104 @@ def _ptr(x) -> int:
 
 _I64x3 = ctypes.c_int64 * 3
 
+# What the rotation table, the norm and rotation and the masked attention ask of tensors, so that none is read as another kind, past
+# its end or on another device than the context's.  Addresses are taken as they are.
+_CTX_DEVICE: dict = {}  # device of every context
 
-def _row_stride(x, name: str) -> int:
-    """Elements from row to row of a bf16 tensor [rows, heads, head_dim] with contiguous heads; 0: contiguous, or an address."""
-    if not hasattr(x, "stride"):
-        return 0
-    if x.element_size() == 2:
+
+class _Kind(set):
+    """Tensor types that an argument may have, as far as they have been met, and the names of all: this module does not import
+    torch."""
+
+    def __init__(self, what, *names):
+        super().__init__()
+        self.what, self.names = what, names
+
+    def meet(self, dtype) -> bool:
+        if str(dtype) not in self.names:
+            return False
+        self.add(dtype)
+        return True
+
+
+_BF16 = _Kind("bf16", "torch.bfloat16", "torch.int16", "torch.uint16")  # the integers: bit patterns
+_FP32 = _Kind("fp32", "torch.float32")
+_INT32 = _Kind("int32", "torch.int32", "torch.uint32")
+
+
+def _check_kind(x, name: str, kind: _Kind) -> None:
+    if x.dtype not in kind and not kind.meet(x.dtype):
+        raise ValueError(f"{name}: a {kind.what} tensor, not {x.dtype}")
+
+
+def _row_stride(x, name: str, shape) -> int:
+    """Elements from row to row of a bf16 tensor [rows, heads, head_dim] with contiguous heads; 0: contiguous."""
+    if x.dtype in _BF16 or _BF16.meet(x.dtype):
         if x.is_contiguous():
             return 0
-        shape, (rows, heads, inner) = x.shape, x.stride()
-        if (inner == 1 or shape[2] == 1) and (heads == shape[2] or shape[1] == 1):
-            return rows if shape[0] > 1 else 0
+        if len(shape) == 3:
+            row, head, one = x.stride()
+            if (one == 1 or shape[2] == 1) and (head == shape[2] or shape[1] == 1):
+                if shape[0] == 1:
+                    return 0
+                if row > 0:  # 0, which an expanded tensor has, would stand for contiguous rows
+                    return row
     raise ValueError(f"{name}: a bf16 tensor [rows, heads, head_dim] whose heads are contiguous")
 
 
-def _array(x, name: str, floating: bool) -> int:
-    """Address of a contiguous device array of 4-byte floats or integers; a tensor of another kind is refused."""
-    if x is not None and hasattr(x, "element_size"):
-        if x.element_size() != 4 or x.is_floating_point() != floating or not x.is_contiguous():
-            raise ValueError(f"{name}: a contiguous {'fp32' if floating else 'int32'} tensor")
-    return _ptr(x)
+def _check_size(name: str, shape, n_rows: int, heads: int, head_dim: int) -> None:
+    """At least n_rows rows of heads * head_dim elements.  A contiguous tensor of other than three dimensions may hold them too."""
+    if len(shape) == 3:
+        rows, h, d = shape
+        if rows >= n_rows and h == heads and d == head_dim:
+            return
+    elif len(shape) < 2 or shape[-1] == heads * head_dim or shape[-2:] == (heads, head_dim):
+        if math.prod(shape) >= n_rows * heads * head_dim:
+            return
+    raise ValueError(f"{name}: {n_rows} rows of {heads} heads of {head_dim} elements, not {tuple(shape)}")
+
+
+def _check_device(name: str, where: int, device) -> None:
+    if where != device and device is not None:  # (the library refuses a call without a context)
+        raise ValueError(f"{name}: on device {where} (-1: the host), the context on {device}")
+
+
+def _operand(x, name: str, n_rows: int, heads, head_dim: int, device, own: bool):
+    """(address, elements from row to row or 0) of queries, keys, values or an output; own: the tensor's strides count.  heads is
+    None in a call that the library refuses."""
+    if not hasattr(x, "stride"):
+        return _ptr(x), 0
+    row = 0
+    if own:
+        shape = x.shape
+        row = _row_stride(x, name, shape)
+        if heads is not None:
+            _check_size(name, shape, n_rows, heads, head_dim)
+    else:
+        _check_kind(x, name, _BF16)
+    where = x.get_device()
+    if where != device:
+        _check_device(name, where, device)
+    return x.data_ptr(), row
+
+
+def _array(x, name: str, kind: _Kind, size: int = 0, device=None) -> int:
+    """Address of a contiguous device array of at least `size` elements; a tensor of another kind is refused."""
+    if x is None:
+        return 0
+    try:
+        dtype = x.dtype
+    except AttributeError:
+        return int(x)
+    if (dtype not in kind and not kind.meet(dtype)) or not x.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {kind.what} tensor")
+    if x.numel() < size:
+        raise ValueError(f"{name}: at least {size} elements, not {x.numel()}")
+    if device is not None:
+        where = x.get_device()
+        if where != device:
+            _check_device(name, where, device)
+    return x.data_ptr()
 
 
 def _cu_array(cu_seqlens) -> np.ndarray:
@@ -283,6 +418,7 @@ def dit_attn_create(device_id: int = 0) -> int:
     rc = lib.dit_attn_create(ctypes.byref(h), int(device_id))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(None))
+    _CTX_DEVICE[int(h.value)] = int(device_id)
     return int(h.value)
 
 
@@ -319,6 +455,7 @@ def dit_attn_last_launch_kernel(ctx) -> int:
 
 def dit_attn_destroy(ctx) -> None:
     if ctx:
+        _CTX_DEVICE.pop(ctx, None)
         load_library().dit_attn_destroy(ctypes.c_void_p(ctx))
 
 
@@ -424,10 +561,21 @@ def dit_attn_sp_unpack_heads(ctx, src, dst, n_rows: int, n_heads: int, head_dim:
     _sp_layout("dit_attn_sp_unpack_heads", ctx, src, dst, n_rows, n_heads, head_dim, sp_degree, stream)
 
 
+_MAX_ROWS = 2 ** 34  # more are refused by the library
+_AXES = struct.Struct("6i").unpack_from  # n_axes, scaling and axis_dim of a RopeSpec
+
+
 def dit_attn_rope_table(ctx, positions, n_rows: int, rope: RopeSpec, table, stream=None) -> None:
     """table[r, pair] = (cos, sin) of the row's positions; positions: device int32 [n_rows, n_axes]; see include/dit_attn.h."""
-    rc = load_library().dit_attn_rope_table(ctx, _array(positions, "positions", False), n_rows, rope, _array(table, "table", True),
-                                            _ptr(stream))
+    n_positions = n_values = 0
+    if rope is not None and n_rows <= _MAX_ROWS:
+        axes, _, *dims = _AXES(rope)
+        size = sum(dims[:axes])
+        if 1 <= axes <= 4 and size <= 128:  # else the library refuses the call
+            n_positions, n_values = n_rows * axes, n_rows * size
+    device = _CTX_DEVICE.get(ctx)
+    rc = load_library().dit_attn_rope_table(ctx, _array(positions, "positions", _INT32, n_positions, device), n_rows, rope,
+                                            _array(table, "table", _FP32, n_values, device), _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 
@@ -435,8 +583,16 @@ def dit_attn_rope_table(ctx, positions, n_rows: int, rope: RopeSpec, table, stre
 def dit_attn_qk_norm_rope(ctx, q, k, n_rows: int, head_dim: int, norm: int, eps: float, table=None, rot_dim: int = 0,
                           layout: int = ROPE_INTERLEAVED, stream=None) -> None:
     """Norm of queries and keys for each head and rotation; q, k: NormHeads, or None for one of them; see include/dit_attn.h."""
-    rc = load_library().dit_attn_qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, _array(table, "table", True), rot_dim, layout,
-                                              _ptr(stream))
+    device, n_values = _CTX_DEVICE.get(ctx), 0
+    if n_rows <= _MAX_ROWS and (head_dim == 128 or head_dim == 64):  # else the library refuses the call
+        if rot_dim <= head_dim:
+            n_values = n_rows * rot_dim
+        if q is not None:
+            q._check(n_rows, head_dim, device)
+        if k is not None:
+            k._check(n_rows, head_dim, device)
+    rc = load_library().dit_attn_qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, _array(table, "table", _FP32, n_values, device),
+                                              rot_dim, layout, _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 
@@ -446,7 +602,9 @@ def dit_attn_masked_varlen_fwd(ctx, q, k, v, cu_seqlens_q, cu_seqlens_k, n_heads
     """Attention with masks, capped scores and a distance bias; see include/dit_attn.h.
 
     q, k, v: bf16 tensors [rows, heads, head_dim] whose rows may be strided, or integer addresses (with row_strides, three
-    numbers of elements, 0: contiguous).  cu_seqlens_k may be None (that of the queries); mask, lse may be None.
+    numbers of elements, 0: contiguous).  cu_seqlens_k may be None (that of the queries); mask, lse may be None.  Tensors of
+    another type, shape or device than the call reads, or too small for it, raise ValueError; with row_strides their type and
+    device are looked at alone.
     """
     lib = load_library()
     cq = _cu_array(cu_seqlens_q)
@@ -457,12 +615,34 @@ def dit_attn_masked_varlen_fwd(ctx, q, k, v, cu_seqlens_q, cu_seqlens_k, n_heads
         raise ValueError("cu_seqlens_q and cu_seqlens_k need n_seqs + 1 entries")
     if mask is not None and mask.n_prefix is not None and mask.n_prefix < n_seqs:
         raise ValueError("mask.prefix needs an entry for every sequence")
-    if row_strides is None:
-        row_strides = (_row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v"))
-    if _row_stride(out, "out") != 0:
+    device, heads, kv_heads, rows, keys = _CTX_DEVICE.get(ctx), None, None, 0, 0
+    if n_seqs >= 0 and (head_dim == 128 or head_dim == 64) and n_heads > 0 and n_kv_heads > 0 and n_heads % n_kv_heads == 0:
+        heads, kv_heads = n_heads, n_kv_heads  # else the library refuses the call
+        rows = cq.item(n_seqs)
+        keys = rows if ck is None else ck.item(n_seqs)
+    own = row_strides is None
+    q_at, q_row = _operand(q, "q", rows, heads, head_dim, device, own)
+    k_at, k_row = _operand(k, "k", keys, kv_heads, head_dim, device, own)
+    v_at, v_row = _operand(v, "v", keys, kv_heads, head_dim, device, own)
+    out_at, out_row = _operand(out, "out", rows, heads, head_dim, device, True)
+    if out_row != 0:
         raise ValueError("out: contiguous rows")
-    rc = lib.dit_attn_masked_varlen_fwd(ctx, _ptr(q), _ptr(k), _ptr(v), _I64x3(*row_strides), cq.__array_interface__["data"][0],
-                                        None if ck is None else ck.__array_interface__["data"][0], n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, _ptr(out), _array(lse, "lse", True), _ptr(stream))
+    if not own:
+        row_strides = _I64x3(*row_strides)
+    elif q_row or k_row or v_row:
+        row_strides = _I64x3(q_row, k_row, v_row)
+    if mask is not None and heads is not None:
+        _, slopes, q_doc, k_doc = mask._held
+        if slopes is not None:
+            _array(slopes, "slopes", _FP32, n_heads, device)
+        if q_doc is not None:
+            _array(q_doc, "q_doc", _INT32, rows, device)
+        if k_doc is not None:
+            _array(k_doc, "k_doc", _INT32, keys, device)
+    # (The boundaries' bytes: an array's address takes longer.)
+    rc = lib.dit_attn_masked_varlen_fwd(ctx, q_at, k_at, v_at, row_strides, cq.tobytes(),
+                                        None if ck is None else ck.tobytes(), n_seqs, n_heads, n_kv_heads, head_dim, scale, mask, out_at,
+                                        _array(lse, "lse", _FP32, rows * heads if heads else 0, device), _ptr(stream))
     if rc != 0:
         raise DitAttnError(rc, dit_attn_last_error(ctx))
 
