@@ -215,7 +215,7 @@ int dit_attn_sp_unpack_heads(dit_attn_ctx* ctx, const void* src, void* dst, int6
  *   rope       HOST, read during the call.
  *   table      DEVICE fp32 [n_rows, sum of axis_dim / 2, 2] (cos, sin), 16-byte aligned.
  * Enqueues one kernel on `stream`; allocates nothing.  Returns DIT_ATTN_OK, _ERR_NULL, _ROPE, _CU_SEQLENS (n_rows < 0), _ALIGN,
- * _LIMIT (over 2^34 rows) or _HIP.
+ * _LIMIT (over 2^34 rows, or more than a launch takes: with 64 pairs 2^29) or _HIP.
  */
 #define DIT_ATTN_ROPE_PLAIN   0
 #define DIT_ATTN_ROPE_LINEAR  1
@@ -253,7 +253,8 @@ int dit_attn_rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_r
  *               rot_dim == 0.
  *   rot_dim     rotated elements of a head, a multiple of 8 up to head_dim; the others are only normed.
  * Enqueues one kernel on `stream`; allocates nothing.  Returns DIT_ATTN_OK, _ERR_NULL, _HEAD_DIM, _N_HEADS, _NORM, _ROPE,
- * _STRIDE, _CU_SEQLENS (n_rows < 0), _ALIGN, _LIMIT or _HIP.
+ * _STRIDE, _CU_SEQLENS (n_rows < 0), _ALIGN, _LIMIT (over 2^34 rows, or more than a launch takes: 2^24 groups of up to four heads
+ * of one side and 2048 / head_dim rows) or _HIP.
  */
 #define DIT_ATTN_NORM_NONE          0
 #define DIT_ATTN_NORM_RMS           1

@@ -72,7 +72,6 @@ int rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_rows, cons
   if (!positions || !table) return fail(ctx, DIT_ATTN_ERR_NULL, "positions and table must be non-NULL");
   if (misaligned(positions, 4) || misaligned(table, 16))
     return fail(ctx, DIT_ATTN_ERR_ALIGN, "positions must be 4-byte, table 16-byte aligned");
-  if (n_rows > (int64_t{1} << 34)) return fail(ctx, DIT_ATTN_ERR_LIMIT, "too many rows");
 
   dit::RopeTableParams p{};
   p.positions = positions;
@@ -81,6 +80,7 @@ int rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_rows, cons
   p.n_axes = r->n_axes;
   p.n_pairs = total / 2;
   p.magnitude = static_cast<float>(r->magnitude);
+  if (n_rows > (int64_t{1} << 34) || dit::rope_table_blocks(p) > dit::kMaxRowBlocks) return fail(ctx, DIT_ATTN_ERR_LIMIT, "too many rows");
   int pair = 0;
   for (int a = 0; a < r->n_axes; ++a)
     for (int j = 0; j < r->axis_dim[a] / 2; ++j, ++pair) {
@@ -152,7 +152,7 @@ int qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const dit_attn
   p.rot_dim = rot_dim;
   p.half = layout == DIT_ATTN_ROPE_HALF ? 1 : 0;
   p.eps = eps;
-  if (n_rows > (int64_t{1} << 34) || dit::qk_norm_rope_blocks(p, head_dim) > 0x7FFFFFFF)
+  if (n_rows > (int64_t{1} << 34) || dit::qk_norm_rope_blocks(p, head_dim) > dit::kMaxRowBlocks)
     return fail(ctx, DIT_ATTN_ERR_LIMIT, "too many rows");
   dit::DeviceGuard guard;
   hipError_t e = guard.enter(ctx->device);

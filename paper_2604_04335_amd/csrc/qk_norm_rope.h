@@ -6,6 +6,7 @@
 namespace dit {
 
 constexpr int kMaxRopePairs = 64;  // head_dim 128
+constexpr int64_t kMaxRowBlocks = 0xFFFFFFFFll / 256;  // a launch takes under 2^32 threads, 256 a workgroup here
 
 struct RopeTableParams {
   const int32_t* positions;  // [n_rows, n_axes]
@@ -19,6 +20,8 @@ struct RopeTableParams {
 };
 // Loads the code of these kernels on the current device, which the first launch would otherwise do.
 hipError_t qk_norm_rope_prepare();
+// Workgroups that a call needs (the caller keeps it at kMaxRowBlocks at most); likewise below.
+int64_t rope_table_blocks(const RopeTableParams& p);
 hipError_t rope_table_launch(const RopeTableParams& p, hipStream_t stream);
 
 enum class HeadNorm : int { kNone = 0, kRms = 1, kLayer = 2 };
@@ -39,7 +42,6 @@ struct QkNormRopeParams {
   int32_t half;             // pairs (j, j + rot_dim / 2) instead of (2j, 2j + 1)
   float eps;
 };
-// Workgroups that a call needs (the caller keeps it under 2^31).
 int64_t qk_norm_rope_blocks(const QkNormRopeParams& p, int head_dim);
 hipError_t qk_norm_rope_launch(const QkNormRopeParams& p, HeadNorm norm, int head_dim, hipStream_t stream);
 

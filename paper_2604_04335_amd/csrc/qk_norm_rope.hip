@@ -53,11 +53,14 @@ __global__ void __launch_bounds__(256) rope_table_kernel(RopeTableParams p) {
   }
 }
 
+int64_t rope_table_blocks(const RopeTableParams& p) {
+  const int64_t rows = (256 / p.n_pairs) * kTableRows;
+  return (p.n_rows + rows - 1) / rows;
+}
+
 hipError_t rope_table_launch(const RopeTableParams& p, hipStream_t stream) {
   if (p.n_rows == 0) return hipSuccess;
-  const int64_t rows = (256 / p.n_pairs) * kTableRows, blocks = (p.n_rows + rows - 1) / rows;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)rope_table_blocks(p)), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
