@@ -240,6 +240,7 @@ int dit_attn_rope_table(dit_attn_ctx* ctx, const int32_t* positions, int64_t n_r
  *     DIT_ATTN_NORM_RMS     y = x * rsqrt(mean(x^2) + eps) * weight + bias
  *     DIT_ATTN_NORM_LAYER   y = (x - mean(x)) * rsqrt(var(x) + eps) * weight + bias       (var: mean of squares)
  *     DIT_ATTN_NORM_NONE    y = x
+ * (means are over the elements of one head: a norm over all heads of a row is another operation)
  * then the first rot_dim elements are turned in pairs, (a, b) -> (a cos - b sin, b cos + a sin) with the row's table entry of
  * the pair, and the result is rounded once to bf16.  Pair j is
  *     DIT_ATTN_ROPE_INTERLEAVED  (2j, 2j + 1)          DIT_ATTN_ROPE_HALF  (j, j + rot_dim / 2)
@@ -281,6 +282,7 @@ int dit_attn_qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const
  *     key j is seen  iff  (not causal, or j <= pos, or j < prefix of the sequence)
  *                     and (no ids, or q_doc of the row == k_doc of the key, and that id is not negative)
  *     out = sum over seen keys exp(s - lse) v_j,     lse = ln sum over seen keys exp(s)
+ * Scores are fp32: a capped one is within 1e-6 of its value, a biased one within a few roundings of the bias.
  * A row that sees no key gets 0 and -inf.  What lies in keys and values that a row does not see (NaN and infinities too) has no
  * effect on it.  So a padded batch gives its padding rows negative ids, several documents of a sequence get an id each (in any
  * order), and text that all of an ordered sequence sees is its prefix.
@@ -288,7 +290,8 @@ int dit_attn_qk_norm_rope(dit_attn_ctx* ctx, const dit_attn_norm_heads* q, const
  *   row_strides HOST, elements from row to row of q, k and v (multiples of 8, at most 2^24; 0: contiguous), or NULL: contiguous.
  *               The heads of a row are contiguous.
  *   cu_seqlens_q, cu_seqlens_k   HOST, as dit_attn_cross_varlen_fwd; cu_seqlens_k may be NULL: keys share the query boundaries.
- *               Any number of sequences.
+ *               Any number of sequences.  The keys of a sequence follow those of the one before it: there is no room between
+ *               caches to grow into, so a program that adds a token to each either moves them or makes a call for each.
  *   n_kv_heads  divides n_heads.      head_dim  64 or 128.      scale  finite.
  *   mask        HOST structure, read during the call, or NULL: every key is seen.
  *   out         DEVICE bf16 [Tq, n_heads, head_dim], contiguous, overlapping no input.  Exactly the rows [0, Tq) are written.

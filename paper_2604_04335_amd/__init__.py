@@ -386,7 +386,7 @@ def _array(x, name: str, kind: _Kind, size: int = 0, device=None) -> int:
         return int(x)
     if (dtype not in kind and not kind.meet(dtype)) or not x.is_contiguous():
         raise ValueError(f"{name}: a contiguous {kind.what} tensor")
-    if x.numel() < size:
+    if size and x.numel() < size:
         raise ValueError(f"{name}: at least {size} elements, not {x.numel()}")
     if device is not None:
         where = x.get_device()

@@ -101,7 +101,8 @@ struct LiveTiles {
 __device__ __forceinline__ constexpr int key_of(int kb, int i) { return 32 * kb + 8 * (i >> 2) + (i & 3); }
 
 // C tanh(s / C) log2(e) of a raw score, as a polynomial where it is small and 1 - 2 / (exp(2 y) + 1) of y = s / C, whose limits
-// need no clamp, where that keeps its relative precision.
+// need no clamp, where that keeps its relative precision: either is within 1e-6 of the score, most of it the roundings of 2 y, the
+// exponential and the reciprocal next to a quarter of C (the polynomial is off by 4e-7).
 __device__ __forceinline__ float small_cap(const MaskedParams& p, float x) {
   const float z = x * x;
   return x * __builtin_fmaf(z, __builtin_fmaf(z, p.poly[2], p.poly[1]), p.poly[0]);
@@ -506,9 +507,13 @@ constexpr int kMaskedWaves = D == 64 && !(CAP && LSE) ? 3 : 2;
 // this one.  Most tiles are touched by no mask; runs of them have a loop of their own, in which a cap and a bias cost their few
 // instructions a score beside the MFMAs.  What else shapes and masks a tile's scores stands between two steps.
 // us on MI355X, with the three parts of a tile in turn / now:  20506 rows x 24 heads, D 128, unmasked 5387 / 4330 (1190 TFLOP/s, the
-// unmasked 128-row kernel 4220), cap 6888 / 5060, bias 6237 / 4810, causal 2603 / 2130;  4352 x 24 x 6, D 64, unmasked 790 / 690,
-// bias 987 / 769, padded documents of three 559 / 412.  Bound by power (1.7 GHz) with both pipes of a SIMD over half busy; the
+// unmasked 128-row kernel 4220), cap 6888 / 5060, bias 6237 / 4580, causal 2603 / 2130;  4352 x 24 x 6, D 64, unmasked 790 / 690,
+// bias 987 / 766, padded documents of three 559 / 393.  Bound by power (1.7 GHz) with both pipes of a SIMD over half busy; the
 // padded documents by vector instructions, half of their tiles being at an edge of a document or around the rows' own places.
+// That cap is of scores under a quarter of it, which take the polynomial alone.  One score past that in 32 rows and 64 keys and the
+// wavefront computes both forms of all of them between two steps, an exponential and a reciprocal each:  unmasked / small / large
+// 4380 / 5150 / 8300 at D 128, 696 / 870 / 1683 at D 64.  Cap and bias together are shaped between two steps too:  5860 with small
+// scores and 8170 with large ones, 1022 and 1598.
 // 128 rows and not 64 or 256: two workgroups of four wavefronts fill a compute unit's registers and 130 of its 160 KB LDS.
 template <class T, bool CAP, bool BIAS, bool LSE>
 __global__ void __attribute__((amdgpu_flat_work_group_size(T::NT, T::NT), amdgpu_waves_per_eu(kMaskedWaves<T::D, CAP, LSE>, kMaskedWaves<T::D, CAP, LSE>)))
