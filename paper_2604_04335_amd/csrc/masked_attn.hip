@@ -1225,7 +1225,11 @@ __global__ void __launch_bounds__(256) masked_join_kernel(MaskedParams p, int32_
   auto add = [&](elems x, int i) {
     const float wi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), i));
 #pragma unroll
-    for (int k = 0; k < D / 64; ++k) acc[k] = __builtin_fmaf(wi, wi != 0.f ? x[k] : 0.f, acc[k]);  // unseen: no weight, unwritten
+    for (int k = 0; k < D / 64; ++k) {
+      // A weight that is 0 in 32 bits keeps what is not finite, as in a call without parts.  (Nothing seen: x is 0.)
+      const bool keep = wi == 0.f && !(__builtin_fabsf(x[k]) < __builtin_inff());
+      acc[k] = keep ? acc[k] + x[k] : __builtin_fmaf(wi, x[k], acc[k]);
+    }
   };
   int i = 0;
   for (; i + 8 <= parts; i += 8) {

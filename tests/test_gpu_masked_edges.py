@@ -42,6 +42,24 @@ def test_values_of_two_keys_that_are_nan_in_turn(ctx, D, few, first):
     assert torch.equal(out[~want].view(torch.int16), clean[~want].view(torch.int16)) and torch.equal(lse, clean_lse)
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_that_are_not_finite_in_a_part_of_no_weight(ctx, D, rows):
+    """Keys in several parts, and a bias that leaves those far away a probability of 0 in 32 bits: their values are seen all the same."""
+    rng = _rng(D + rows)
+    n, H = 5000, 2
+    q, k, v = to_dev(_bf16(rng, rows, H, D)), to_dev(_bf16(rng, n, H, D)), to_dev(_bf16(rng, n, H, D))
+    mask = da.AttnMask(slopes=torch.full((H,), 2.0, device="cuda"))
+    clean, clean_lse = _run_masked(ctx, q, k, v, _cu([rows]), _cu([n]), D ** -0.5, mask)
+    v[3, 0, 5] = float("nan")
+    v[900, 1, 7] = float("nan")
+    out, lse = _run_masked(ctx, q, k, v, _cu([rows]), _cu([n]), D ** -0.5, mask)
+    want = torch.zeros((rows, H, D), dtype=torch.bool, device="cuda")
+    want[:, 0, 5] = want[:, 1, 7] = True
+    assert torch.equal(torch.isnan(out), want)
+    assert torch.equal(out[~want].view(torch.int16), clean[~want].view(torch.int16)) and torch.equal(lse, clean_lse)
+
+
 def test_an_unseen_value_costs_nothing(ctx):
     """A key of another document whose value is NaN, at every place of a tile: the call takes as long as for any other place, not a
     walk over all keys."""
