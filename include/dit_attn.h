@@ -311,7 +311,7 @@ typedef struct dit_attn_mask {
   float softcap;               /* C, or 0: scores are not capped */
   const int32_t* prefix;       /* HOST [n_seqs], not negative, with causal = 1; or NULL: 0 */
   const float* slopes;         /* DEVICE fp32 [n_heads], or NULL: no bias */
-  const int32_t* q_doc;        /* DEVICE int32 [Tq] and [Tk], or both NULL */
+  const int32_t* q_doc;        /* DEVICE int32 [Tq] and [Tk], or both NULL (one of no elements may be NULL too) */
   const int32_t* k_doc;
 } dit_attn_mask;
 int dit_attn_masked_varlen_fwd(dit_attn_ctx* ctx,

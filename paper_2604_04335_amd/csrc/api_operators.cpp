@@ -275,7 +275,10 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
   if (m.prefix)
     for (int32_t i = 0; i < n_seqs; ++i)
       if (m.prefix[i] < 0) return fail(ctx, DIT_ATTN_ERR_MASK, "prefix must not be negative");
-  if ((m.q_doc == nullptr) != (m.k_doc == nullptr)) return fail(ctx, DIT_ATTN_ERR_MASK, "q_doc and k_doc come together");
+  const int64_t total_q = n_seqs > 0 ? cu_q[n_seqs] : 0, total_k = n_seqs > 0 ? cu_k[n_seqs] : 0;
+  // (An array of no ids may have no address.)
+  if ((m.q_doc || m.k_doc) && ((!m.q_doc && total_q > 0) || (!m.k_doc && total_k > 0)))
+    return fail(ctx, DIT_ATTN_ERR_MASK, "q_doc and k_doc come together");
   int64_t strides[3];
   for (int i = 0; i < 3; ++i) {
     const int64_t row = static_cast<int64_t>(i == 0 ? n_heads : n_kv_heads) * head_dim;
@@ -283,7 +286,6 @@ int masked_forward(dit_attn_ctx* ctx, const void* q, const void* k, const void* 
     if (strides[i] < row || strides[i] % 8 != 0 || strides[i] > (int64_t{1} << 24))
       return fail(ctx, DIT_ATTN_ERR_STRIDE, "row strides must be multiples of 8 elements, hold a row's heads and be at most 2^24");
   }
-  const int64_t total_q = n_seqs > 0 ? cu_q[n_seqs] : 0, total_k = n_seqs > 0 ? cu_k[n_seqs] : 0;
   if (total_q == 0) return DIT_ATTN_OK;
   if (!q || !out || (total_k > 0 && (!k || !v))) return fail(ctx, DIT_ATTN_ERR_NULL, "q, k, v and out must be non-NULL");
   if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16))

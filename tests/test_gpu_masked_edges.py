@@ -91,6 +91,22 @@ def test_an_unseen_value_costs_nothing(ctx):
         assert time_of(place) < 3 * usual, place
 
 
+@pytest.mark.parametrize("rows", [3, 200])
+def test_ids_of_no_keys_and_of_no_rows(ctx, rows):
+    """Empty tensors have no address: rows with ids against no keys at all, and keys with ids for no rows."""
+    rng = _rng(rows)
+    H, D = 2, 64
+    q, none = to_dev(_bf16(rng, rows, H, D)), torch.empty((0, H, D), dtype=torch.bfloat16, device="cuda")
+    ids, no_ids = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    out, lse = _run_masked(ctx, q, none, none, _cu([rows]), _cu([0]), 0.1, da.AttnMask(q_doc=ids, k_doc=no_ids))
+    assert not bool(out.any()) and bool((lse == float("-inf")).all())
+    _run_masked(ctx, none, q, q, _cu([0]), _cu([rows]), 0.1, da.AttnMask(q_doc=no_ids, k_doc=ids))
+    _run_masked(ctx, none, none, none, _cu([0]), None, 0.1, da.AttnMask(q_doc=no_ids, k_doc=no_ids))
+    for mask in (da.AttnMask(k_doc=ids), da.AttnMask(q_doc=no_ids, k_doc=ids), da.AttnMask(q_doc=ids)):
+        with pytest.raises((da.DitAttnError, ValueError)):
+            _run_masked(ctx, q, q, q, _cu([rows]), None, 0.1, mask)
+
+
 BIAS_CASES = [
     # q lens, k lens (None: the same), H, G, D, options: runs that begin and end at documents, behind the rows and before them
     ([1500], None, 2, 2, 64, dict(bias=True, docs=2, pad=101)),
