@@ -131,6 +131,7 @@ class NormHeads(ctypes.Structure):
     weight, bias: fp32 [head_dim] or None."""
     _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64),
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("n_heads", ctypes.c_int32)]
+    _needs = (None, None, None, None)  # of a structure whose fields were filled in one by one
 
     def __init__(self, x, out, weight=None, bias=None, n_heads=None, row_stride=None, out_row_stride=None):
         # What a call has to agree with: the shapes of tensors whose strides are their own, the elements of weight and bias, and the
@@ -199,6 +200,7 @@ class AttnMask(ctypes.Structure):
     device int32 [Tq], [Tk]."""
     _fields_ = [("causal", ctypes.c_int32), ("softcap", ctypes.c_float), ("prefix", ctypes.POINTER(ctypes.c_int32)),
                 ("slopes", ctypes.c_void_p), ("q_doc", ctypes.c_void_p), ("k_doc", ctypes.c_void_p)]
+    n_prefix, _held = None, (None, None, None, None)  # of a structure whose fields were filled in one by one
 
     def __init__(self, causal=False, prefix=None, softcap=0.0, slopes=None, q_doc=None, k_doc=None):
         self.n_prefix = None
@@ -568,7 +570,7 @@ _AXES = struct.Struct("6i").unpack_from  # n_axes, scaling and axis_dim of a Rop
 def dit_attn_rope_table(ctx, positions, n_rows: int, rope: RopeSpec, table, stream=None) -> None:
     """table[r, pair] = (cos, sin) of the row's positions; positions: device int32 [n_rows, n_axes]; see include/dit_attn.h."""
     n_positions = n_values = 0
-    if rope is not None and n_rows <= _MAX_ROWS:
+    if isinstance(rope, RopeSpec) and n_rows <= _MAX_ROWS:
         axes, _, *dims = _AXES(rope)
         size = sum(dims[:axes])
         if 1 <= axes <= 4 and size <= 128:  # else the library refuses the call
@@ -587,9 +589,9 @@ def dit_attn_qk_norm_rope(ctx, q, k, n_rows: int, head_dim: int, norm: int, eps:
     if n_rows <= _MAX_ROWS and (head_dim == 128 or head_dim == 64):  # else the library refuses the call
         if rot_dim <= head_dim:
             n_values = n_rows * rot_dim
-        if q is not None:
+        if isinstance(q, NormHeads):
             q._check(n_rows, head_dim, device)
-        if k is not None:
+        if isinstance(k, NormHeads):
             k._check(n_rows, head_dim, device)
     rc = load_library().dit_attn_qk_norm_rope(ctx, q, k, n_rows, head_dim, norm, eps, _array(table, "table", _FP32, n_values, device),
                                               rot_dim, layout, _ptr(stream))

@@ -171,3 +171,13 @@ def test_contexts_are_known_by_their_device(monkeypatch):
 def test_boundaries_of_other_types_and_strides():
     passes(masked, cu_q=np.array([0, 3, 8], np.int64))
     passes(masked, cu_q=np.array([0, 9, 3, 9, 8, 9], np.int32)[::2])
+
+
+def test_structures_by_address_and_filled_in_one_by_one():
+    import ctypes
+
+    side = da.NormHeads(4096, 4096, n_heads=2)
+    for x in (side, ctypes.byref(side), da.NormHeads.from_buffer_copy(bytes(side))):
+        passes(da.dit_attn_qk_norm_rope, None, x, None, 8, 64, da.NORM_RMS, 1e-6)
+    passes(da.dit_attn_rope_table, None, 4096, 8, ctypes.byref(da.RopeSpec([16])), 4096)
+    passes(masked, mask=da.AttnMask.from_buffer_copy(bytes(da.AttnMask(causal=True))))
